@@ -382,6 +382,147 @@ int32_t dsbd_build_forest(int32_t n_prompts, int32_t n_roots, int32_t gamma, int
                           const dsbd_forest_out* out, int32_t* fault, void* stream);
 
 /*
+ * ---- The rows of a projection on their way into the step, paged caches, rules on logits.  What the paper takes for
+ * granted of the models: the calls below prepare what dsbd_forest_attention, dsbd_draft_layer and dsbd_verify_forest
+ * read, and run the passes around them (prompts in chunks, the small model's single tokens) on the same caches.
+ */
+
+/* element types */
+#define DSBD_BF16 0
+#define DSBD_F16  1
+#define DSBD_F32  2
+
+/* Rows [n,H,D] of a tensor: channel d of head h of row i at ptr[i*token_stride + h*head_stride + d] (elements), so a slice of a
+ * fused projection or a head-major tensor needs no copy.  ptr 16-byte aligned, strides multiples of 8 and not negative. */
+typedef struct dsbd_rows {
+  void*   ptr;
+  int64_t token_stride, head_stride;
+} dsbd_rows;
+
+/*
+ * What happens to the rows of q and k before the attention, in this order, each part optional:
+ *   norm     every head by itself: x := x / sqrt(mean(x^2) + eps) * weight, over its D channels
+ *   rotation of the first rot_dim channels by the row's position: pair i turned by the angle position * inv_freq[i], cosine
+ *            and sine times rot_scale.  A pair is the channels (i, i + rot_dim/2), or (2i, 2i+1) with `interleaved`.
+ * Sums, products and angles' sines in fp32, angles in fp64 (exact to 1e-7 of a turn up to position 2^31), one rounding at
+ * the end.  Scaled rotations (interpolated, by parts, ...) are other tables inv_freq with their rot_scale.
+ */
+typedef struct dsbd_qk_prep {
+  const void*   q_weight;     /* type of the rows, [D], or [Hq,D] with per_head; NULL: 1                    */
+  const void*   k_weight;     /* [D] or [Hkv,D]; NULL: 1                                                    */
+  const double* inv_freq;     /* [rot_dim/2] radians per position; may be NULL if rot_dim == 0              */
+  float         eps;          /* >= 0                                                                       */
+  float         rot_scale;
+  int32_t       rot_dim;      /* 0 (no rotation) .. D, a multiple of 16                                     */
+  int32_t       norm;         /* 0: none (the weights are then not read)                                    */
+  int32_t       per_head;     /* weights hold a vector per head                                             */
+  int32_t       interleaved;
+} dsbd_qk_prep;
+
+/*
+ * Rows of q, k and v as dsbd_forest_attention wants them (q, k_tree, v_tree): q and k through `prep` at positions[i], v
+ * copied.  q [n,Hq,D], k and v [n,Hkv,D] of type DSBD_BF16 or DSBD_F16; each of q, k, v may be NULL together with its output.
+ * An output may be its own input (same pointer and strides); apart from that outputs overlap nothing.
+ * Supported: D a multiple of 16 up to 256.  positions: int32, any value (negative ones turn backwards).
+ */
+int32_t dsbd_qk_norm_rope(int32_t n_rows, int32_t Hq, int32_t Hkv, int32_t D, int32_t dtype,
+                          const dsbd_rows* q, const dsbd_rows* k, const dsbd_rows* v, const int32_t* positions,
+                          const dsbd_qk_prep* prep,
+                          const dsbd_rows* q_out, const dsbd_rows* k_out, const dsbd_rows* v_out, void* stream);
+
+/*
+ * Keys and values in pages: token t of sequence s lives in page page_table[s*table_stride + t / page_size], slot
+ * t % page_size; element (slot, kv-head g, channel d) of page p at k_pages[p*page_stride + slot*token_stride +
+ * g*head_stride + d].  Sequences may share pages (the beams of a prompt share the prompt's); a page that receives tokens
+ * belongs to one sequence.  One page per sequence is a contiguous cache: what dsbd_kv points into can be read and
+ * written through this struct as well.
+ * A call takes a chunk of new tokens for every sequence: rows q_off[s] .. q_off[s+1]-1 of its row arrays are the tokens
+ * ctx_len[s], ctx_len[s]+1, .. of sequence s (any number of them, none too).  Rows in front of q_off[0] and from
+ * q_off[n_seqs] on (padding) are neither read nor written.
+ */
+typedef struct dsbd_paged_kv {
+  void*          k_pages;
+  void*          v_pages;
+  const int32_t* page_table;       /* [n_seqs,table_stride]                                                  */
+  const int32_t* ctx_len;          /* [n_seqs] tokens in front of the new ones                               */
+  const int32_t* q_off;            /* [n_seqs+1] ascending                                                   */
+  int64_t        page_stride, token_stride, head_stride;   /* elements, multiples of 8                       */
+  int32_t        n_pages, page_size, table_stride, n_seqs;
+  /* host-side bounds on the device data, checked on the device (DSBD_FAULT_BOUNDS): */
+  int32_t        max_new;          /* >= new tokens of every sequence                                        */
+  int32_t        max_len;          /* >= ctx_len + new tokens of every sequence                              */
+} dsbd_paged_kv;
+
+/*
+ * Writes the new tokens' keys and values into their pages, k through `prep` on the way; q (may be NULL, with q_out) goes
+ * through `prep` to dense rows in the same launch.  positions: NULL (a token's position is its index in the sequence) or
+ * [n_rows] (the nodes of a tree: ctx_len + depth).  prep: NULL copies.
+ * Device-side problems raise DSBD_FAULT_BOUNDS: lengths outside the bounds, a page index outside [0, n_pages), tokens
+ * behind the table's end; those tokens are not stored (their rows of q are written all the same).
+ */
+int32_t dsbd_paged_append(const dsbd_paged_kv* cache, int32_t n_rows, int32_t Hq, int32_t Hkv, int32_t D, int32_t dtype,
+                          const dsbd_rows* q, const dsbd_rows* k, const dsbd_rows* v, const int32_t* positions,
+                          const dsbd_qk_prep* prep, const dsbd_rows* q_out, int32_t* fault, void* stream);
+
+/*
+ * Attention of the new tokens over their sequences' pages, which hold the new tokens' own keys and values already:
+ * softmax(scale * q.k) v over the keys a row sees, query head h with KV head h / (Hq/Hkv).  A row sees all tokens in front
+ * of the chunk and, of the chunk itself, the tokens up to its own (causal), or, with anc_mask, token j where bit j of
+ * its mask is set (the ancestor bitmaps that dsbd_forest_attention writes; at most 64 new tokens a sequence then).
+ *   q     [n_rows,Hq,D] DSBD_BF16 or DSBD_F16, the pages' type; out the same; lse [n_rows,Hq] f32 natural logarithm, or NULL
+ *   scale <= 0 selects 1/sqrt(D)
+ * A row that sees nothing gets 0 and a lse of -Inf.  Slots behind a sequence's last token are never used, whatever they
+ * hold, and neither is what a row does not see, NaN and Inf among it.
+ * Sequences with lengths outside the bounds raise DSBD_FAULT_BOUNDS and get rows of 0 and -Inf; so do, for the tokens of
+ * that page alone (they count as not there), page indices outside [0, n_pages).
+ * Supported: D = 128 or 64, Hq % Hkv == 0.
+ * Workspace: partial results of the sequences that are split, by the numbers in the arguments alone (not max_len).  Calls with
+ * enough rows to fill the device split nothing and need the least, 256 bytes.
+ */
+size_t dsbd_paged_attention_workspace_bytes(const dsbd_paged_kv* cache, int32_t n_rows, int32_t Hq, int32_t Hkv, int32_t D);
+int32_t dsbd_paged_attention(const dsbd_paged_kv* cache, int32_t n_rows, int32_t Hq, int32_t Hkv, int32_t D, int32_t dtype,
+                             const dsbd_rows* q, float scale, const uint64_t* anc_mask, const dsbd_rows* out, float* lse,
+                             void* workspace, size_t workspace_bytes, int32_t* fault, void* stream);
+
+/* What a row of logits goes through before it is sampled from; every array may be NULL. */
+typedef struct dsbd_logit_rules {
+  /* The text of a beam: its tokens in front of the tree's root, then the nodes of the row's path (root first, the row's
+   * node last).  The first prompt_len tokens of the text are the prompt, the others were generated. */
+  const int32_t*  hist;          /* [n_hist]                                                                  */
+  const int32_t*  hist_off;      /* [n_trees+1] ascending: tokens in front of tree b's root                   */
+  const int32_t*  prompt_len;    /* [n_trees]; NULL: 0                                                        */
+  /* [n_prompts] each */
+  const float*    repetition;    /* > 0: a token of the text: z > 0 ? z / r : z * r                           */
+  const float*    frequency;     /* z -= frequency * (times the token was generated)                          */
+  const float*    presence;      /* z -= presence, if it was generated                                        */
+  const float*    temperature;   /* > 0: z /= temperature, behind the biases                                  */
+  /* biases: prompt p adds bias_value[i] to token bias_token[i], i in bias_off[p] .. bias_off[p+1]-1; of several entries
+   * for one token the last counts */
+  const int32_t*  bias_off;      /* [n_prompts+1] ascending, within [0, n_bias]                               */
+  const int32_t*  bias_token;
+  const float*    bias_value;
+  /* grammar masks: bit v % 32 of word v / 32 clear = token v is not allowed (-Inf) */
+  const uint32_t* mask;          /* [n_masks,mask_stride], mask_stride >= (V+31)/32 words                     */
+  const int32_t*  mask_row;      /* [n_rows] a row's mask, negative: none; NULL: row i has mask i             */
+  int64_t         mask_stride;
+  int32_t         n_masks, n_hist, n_bias;
+} dsbd_logit_rules;
+
+/*
+ * Rows of logits through the rules, in the order repetition, frequency, presence, bias, temperature, mask, in fp32:
+ * what dsbd_verify_forest (both models) and dsbd_draft_layer read, -Inf at the tokens a grammar excludes.
+ * Row i belongs to node i, or to node row_node[i] (the nodes of one layer, as dsbd_build_forest lists them); forest->token
+ * is needed.  logits [n_rows,V] of type DSBD_F32, DSBD_BF16 or DSBD_F16, rows logits_stride elements apart; out [n_rows,V]
+ * f32, rows out_stride apart, may be `logits` itself (f32, same stride).
+ * Device-side problems: trees as in dsbd_forest_attention, a row_node outside the forest (DSBD_FAULT_TOPOLOGY: the row
+ * is copied), token ids outside [0, V) (DSBD_FAULT_TOKEN: ignored), offsets or a mask_row outside their arrays, a
+ * repetition or temperature that is not above 0 (DSBD_FAULT_BOUNDS: that rule is left out).
+ */
+int32_t dsbd_process_logits(const dsbd_forest* forest, const int32_t* row_node, int32_t n_rows, int32_t V, int32_t dtype,
+                            const void* logits, int64_t logits_stride, const dsbd_logit_rules* rules, float* out,
+                            int64_t out_stride, int32_t* fault, void* stream);
+
+/*
  * Tuning overrides (no counterpart in the paper).  The library reads its DSBD_* environment variables (numbers of
  * KV splits and of workgroups per prompt, chunk sizes, the bound of the layer kernel's waits, test hooks) ONCE per
  * process, at the first call that needs them; dsbd_reload_knobs() reads them again.  Host call, no GPU work.

@@ -4,6 +4,7 @@ The structures mirror include/dsbd.h field by field.  Tensors are torch CUDA(HIP
 data pointers and the current stream's handle are passed through unchanged.
 """
 import ctypes as C
+import math
 import os
 from dataclasses import dataclass
 from typing import List, Optional
@@ -80,6 +81,29 @@ class _KVDst(C.Structure):
     _fields_ = [("k_ptr", C.c_void_p), ("v_ptr", C.c_void_p), ("len", C.c_void_p), ("capacity", C.c_int32)]
 
 
+class _Rows(C.Structure):
+    _fields_ = [("ptr", C.c_void_p), ("token_stride", C.c_int64), ("head_stride", C.c_int64)]
+
+
+class _QKPrep(C.Structure):
+    _fields_ = [("q_weight", C.c_void_p), ("k_weight", C.c_void_p), ("inv_freq", C.c_void_p), ("eps", C.c_float),
+                ("rot_scale", C.c_float), ("rot_dim", C.c_int32), ("norm", C.c_int32), ("per_head", C.c_int32),
+                ("interleaved", C.c_int32)]
+
+
+class _PagedKV(C.Structure):
+    _fields_ = [("k_pages", C.c_void_p), ("v_pages", C.c_void_p), ("page_table", C.c_void_p), ("ctx_len", C.c_void_p),
+                ("q_off", C.c_void_p), ("page_stride", C.c_int64), ("token_stride", C.c_int64), ("head_stride", C.c_int64),
+                ("n_pages", C.c_int32), ("page_size", C.c_int32), ("table_stride", C.c_int32), ("n_seqs", C.c_int32),
+                ("max_new", C.c_int32), ("max_len", C.c_int32)]
+
+
+class _LogitRules(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("hist", "hist_off", "prompt_len", "repetition", "frequency", "presence", "temperature",
+                                          "bias_off", "bias_token", "bias_value", "mask", "mask_row")] + [
+        ("mask_stride", C.c_int64), ("n_masks", C.c_int32), ("n_hist", C.c_int32), ("n_bias", C.c_int32)]
+
+
 def lib_path():
     return os.path.join(_HERE, "libdsbd.so")
 
@@ -132,6 +156,20 @@ def load_library():
     lib.dsbd_verify_forest_static.restype = C.c_int32
     lib.dsbd_verify_forest_static.argtypes = [C.POINTER(_Forest), C.POINTER(_VerifyIn), C.POINTER(_Params),
                                               C.POINTER(_VerifyOut), C.c_void_p, C.c_void_p]
+    lib.dsbd_qk_norm_rope.restype = C.c_int32
+    lib.dsbd_qk_norm_rope.argtypes = ([C.c_int32] * 5 + [C.POINTER(_Rows)] * 3 + [C.c_void_p, C.POINTER(_QKPrep)] + [C.POINTER(_Rows)] * 3
+                                      + [C.c_void_p])
+    lib.dsbd_paged_append.restype = C.c_int32
+    lib.dsbd_paged_append.argtypes = ([C.POINTER(_PagedKV)] + [C.c_int32] * 5 + [C.POINTER(_Rows)] * 3
+                                      + [C.c_void_p, C.POINTER(_QKPrep), C.POINTER(_Rows), C.c_void_p, C.c_void_p])
+    lib.dsbd_paged_attention_workspace_bytes.restype = C.c_size_t
+    lib.dsbd_paged_attention_workspace_bytes.argtypes = [C.POINTER(_PagedKV)] + [C.c_int32] * 4
+    lib.dsbd_paged_attention.restype = C.c_int32
+    lib.dsbd_paged_attention.argtypes = ([C.POINTER(_PagedKV)] + [C.c_int32] * 5 + [C.POINTER(_Rows), C.c_float, C.c_void_p, C.POINTER(_Rows)]
+                                         + [C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p, C.c_void_p])
+    lib.dsbd_process_logits.restype = C.c_int32
+    lib.dsbd_process_logits.argtypes = [C.POINTER(_Forest), C.c_void_p, C.c_int32, C.c_int32, C.c_int32, C.c_void_p, C.c_int64,
+                                        C.POINTER(_LogitRules), C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p]
     lib.dsbd_stream_read_probe.restype = C.c_int32
     lib.dsbd_stream_read_probe.argtypes = [C.c_void_p, C.c_size_t, C.c_int32, C.POINTER(C.c_float), C.c_void_p]
     lib.dsbd_reload_knobs.restype = None
@@ -560,6 +598,132 @@ def dsbd_build_forest(root_off, layer_parent, layer_token, root_token=None, *, n
     f = Forest(tree_prompt, tree_off, parent, token, rank, n_prompts=root_off.numel() - 1,
                max_tree_nodes=64, max_depth=gamma, max_prompt_trees=int(max_prompt_trees), device=dev)
     return f, node_of_root, node_of, mx, fault
+
+
+DSBD_BF16, DSBD_F16, DSBD_F32 = 0, 1, 2
+
+
+def rope_inv_freq(rot_dim, base=10000.0, scaling=None, factor=1.0, *, orig_len=0, low=1.0, high=32.0, device="cuda"):
+    """Frequencies of a rotation (radians per position, f64 [rot_dim/2]) and the factor on its cosines and sines.
+    base ** (-2i / rot_dim), and for contexts `factor` times as long as the trained `orig_len`:
+      "linear"    positions are interpolated: every frequency divided by the factor
+      "base"      the base grows to base * factor ** (rot_dim / (rot_dim - 2)): the slowest pair is divided by the factor, the
+                  fastest is left as it is
+      "by_parts"  pairs that make at least `high` turns over orig_len positions are left, those with at most `low` are
+                  divided, a linear ramp over the pair's number between them; cosines and sines times 0.1 ln(factor) + 1
+      "by_turns"  the same ends, with a ramp over the number of turns itself, and no factor on cosines and sines"""
+    if rot_dim < 2 or rot_dim % 2 or not base > 1.0 or not factor > 0.0:
+        raise ValueError("rope_inv_freq: rot_dim is even and positive, base above 1, factor above 0")
+    i = torch.arange(rot_dim // 2, dtype=torch.float64)
+    if scaling == "base":
+        if rot_dim < 4:
+            raise ValueError("rope_inv_freq: the base of a single pair has no effect")
+        base = base * factor ** (rot_dim / (rot_dim - 2))
+    f = base ** (-2.0 * i / rot_dim)
+    scale = 1.0
+    if scaling == "linear":
+        f = f / factor
+    elif scaling in ("by_parts", "by_turns"):
+        if orig_len < 1 or not 0.0 < low < high:
+            raise ValueError("rope_inv_freq: %s needs orig_len and 0 < low < high" % scaling)
+        if scaling == "by_parts":
+            pair = lambda turns: rot_dim * math.log(orig_len / (2 * math.pi * turns)) / (2 * math.log(base))
+            lo, hi = max(0, math.floor(pair(high))), min(rot_dim - 1, math.ceil(pair(low)))
+            keep = 1.0 - ((i - lo) / max(hi - lo, 1e-3)).clamp(0.0, 1.0)
+            scale = 0.1 * math.log(factor) + 1.0 if factor > 1.0 else 1.0
+        else:
+            keep = ((orig_len * f / (2 * math.pi) - low) / (high - low)).clamp(0.0, 1.0)
+        f = f / factor * (1.0 - keep) + f * keep
+    elif scaling not in (None, "base"):
+        raise ValueError("rope_inv_freq: unknown scaling %r" % (scaling,))
+    return f.to(device), scale
+
+
+class QKPrep:
+    """What the rows of q and k go through: a norm of every head (weights of the rows' type, [D], or [H,D] for a vector per
+    head), then the rotation of the first 2 * len(inv_freq) channels.  inv_freq: f64 (rope_inv_freq)."""
+
+    def __init__(self, norm=False, q_weight=None, k_weight=None, eps=1e-6, inv_freq=None, rot_scale=1.0, interleaved=False):
+        self.norm, self.q_weight, self.k_weight, self.eps = bool(norm), q_weight, k_weight, float(eps)
+        self.inv_freq, self.rot_scale, self.interleaved = inv_freq, float(rot_scale), bool(interleaved)
+
+
+def _call(fn, dev, stream, fault, args):
+    """The native call on `stream` (default: the current stream of the tensors' device), with that device current and what the
+    call allocates belonging to that stream.  args(fault, raw stream)."""
+    if dev.type == "cuda" and (stream is not None or (dev.index is not None and dev.index != torch._C._cuda_getDevice())):
+        with torch.cuda.stream(stream) if stream is not None else torch.cuda.device(dev):
+            return _call(fn, dev, None, fault, args)
+    raw = 0
+    if dev.type == "cuda":
+        raw = torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
+    if fault is None:
+        fault = _fault_word(dev) if dev.type == "cuda" else torch.zeros(1, dtype=torch.int32)
+    out = getattr(_host or _native(), fn)(*args(fault, raw))
+    if type(out) is int:
+        raise DsbdError(out, "dsbd_" + fn)
+    return out, fault
+
+
+def dsbd_qk_norm_rope(q, k, positions, prep, v=None, q_out=None, k_out=None, v_out=None, stream=None):
+    """Rows q [N,Hq,D], k (and v) [N,Hkv,D] (bf16 or f16, any strides over rows and heads; each may be None): norm and rotation
+    of q and k at positions i32[N], v copied.  Returns (q_out, k_out, v_out), packed unless given; an output may be its input."""
+    dev = next(t for t in (q, k, v) if t is not None).device
+    out, _ = _call("qk_norm_rope", dev, stream, False, lambda _, s: (q, k, v, positions, prep, q_out, k_out, v_out, s))
+    return out
+
+
+class PagedKV:
+    """A paged cache and a chunk of new tokens for each of its sequences.  k_pages / v_pages [n_pages, page, Hkv, D] (or
+    [n_pages, Hkv, page, D] with head_major), page_table i32 [n_seqs, pages], ctx_len i32 [n_seqs] tokens in front of the
+    chunk, q_off i32 [n_seqs+1] the chunk's rows; max_new and max_len bound the new tokens and all tokens of a sequence."""
+
+    def __init__(self, k_pages, v_pages, page_table, ctx_len, q_off, *, max_new, max_len, head_major=False):
+        dev = k_pages.device
+        self.k_pages, self.v_pages = k_pages, v_pages
+        self.page_table, self.ctx_len, self.q_off = _i32(page_table, dev), _i32(ctx_len, dev), _i32(q_off, dev)
+        self.max_new, self.max_len, self.head_major = int(max_new), int(max_len), bool(head_major)
+
+
+def dsbd_paged_append(cache: PagedKV, k, v, q=None, positions=None, prep: QKPrep = None, q_out=None, fault=None, stream=None):
+    """Writes the chunk's k and v rows [N,Hkv,D] into their pages, k through `prep` at positions i32[N] (default: the tokens'
+    places in their sequences); q [N,Hq,D] goes through `prep` to q_out.  Returns (q_out or None, fault i32[1])."""
+    return _call("paged_append", k.device, stream, fault, lambda f, s: (cache, k, v, q, positions, prep, q_out, f, s))
+
+
+def dsbd_paged_attention_workspace_bytes(cache: PagedKV, n_rows, Hq):
+    return int(_native().paged_attention_workspace_bytes(cache, int(n_rows), int(Hq)))
+
+
+def dsbd_paged_attention(cache: PagedKV, q, scale=0.0, anc_mask=None, out=None, lse=None, want_lse=True, workspace=None,
+                         fault=None, stream=None):
+    """Attention of the chunk's rows q [N,Hq,D] over the pages, which hold the chunk's own keys and values: causal, or the
+    nodes of a tree with anc_mask i64/u64 [N].  Returns (out [N,Hq,D], lse f32 [N,Hq] or None, fault i32[1])."""
+    out, fault = _call("paged_attention", q.device, stream, fault,
+                       lambda f, s: (cache, q, scale, anc_mask, out, lse, want_lse, workspace, f, s))
+    if not out:
+        raise DsbdError(-2, "dsbd_paged_attention_workspace_bytes")
+    return out[0], out[1], fault
+
+
+class LogitRules:
+    """What rows of logits go through: penalties on the tokens of a beam's text, biases, temperature, grammar masks.
+    hist i32 / hist_off i32[n_trees+1]: the tokens in front of each tree's root; prompt_len i32[n_trees]: how many of the
+    text's tokens are the prompt; repetition, frequency, presence, temperature f32[n_prompts]; bias_off i32[n_prompts+1],
+    bias_token i32, bias_value f32; mask i32 [n_masks, >= ceil(V/32)] (bit set: allowed), mask_row i32[n_rows] (negative: none)."""
+
+    def __init__(self, hist=None, hist_off=None, prompt_len=None, repetition=None, frequency=None, presence=None, temperature=None,
+                 bias_off=None, bias_token=None, bias_value=None, mask=None, mask_row=None):
+        self.hist, self.hist_off, self.prompt_len = hist, hist_off, prompt_len
+        self.repetition, self.frequency, self.presence, self.temperature = repetition, frequency, presence, temperature
+        self.bias_off, self.bias_token, self.bias_value = bias_off, bias_token, bias_value
+        self.mask, self.mask_row = mask, mask_row
+
+
+def dsbd_process_logits(forest: Forest, logits, rules: LogitRules, row_node=None, out=None, fault=None, stream=None):
+    """Rows of logits [R,V] (f32, bf16 or f16) of the forest's nodes, or of the nodes row_node i32[R], through the rules.
+    Returns (out f32 [R,V], fault i32[1]); out may be `logits` itself."""
+    return _call("process_logits", logits.device, stream, fault, lambda f, s: (forest, logits, rules, row_node, out, f, s))
 
 
 def dsbd_stream_read_probe(buf: torch.Tensor, reps: int = 10, stream=None) -> float:

@@ -1,0 +1,540 @@
+// Attention of a chunk of new tokens over a paged cache (dsbd_paged_attention).
+//
+// The rows of a KV head of one sequence are its new tokens times the query heads of the group, token-major: row r is token
+// r / group, head r % group, so whatever shares keys shares a workgroup.  A unit is (sequence, block of rows, KV head); the
+// keys that a unit sees are cut into parts where there are fewer units than the device takes at once, and the parts' results
+// (unnormalised output, reference exponent, sum) are joined by a second kernel.
+//
+// Wave-private kernel: each of the 4 waves takes 32-token steps of its own from memory through registers into its LDS tiles;
+//   S^T = K Q^T    MFMA 16x16x32, Q^T held in registers: a lane owns one query row, so the softmax stays inside the lane;
+//   O^T += V^T P^T MFMA 16x16x32, P^T from the registers of S^T, V^T by the transposing LDS read.
+#include "common.h"
+#include "paged.h"
+#include "wave_f64.h"
+#include <algorithm>
+
+namespace {
+
+#define PA_BLOCK 256
+#define PA_STEP 32                 // tokens per wave step
+#define PA_SLOTS 512               // workgroups of the wave-private kernel that the device holds (70 KB of LDS each)
+#define PA_MIN_STEPS 4             // steps that a part has at least
+
+typedef float floatx4 __attribute__((ext_vector_type(4)));
+typedef short v4i16 __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) v4i16 lds_v4i16;
+typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(1))) u32x4 gvec;
+
+// The two element types.  Softmax numerators are rounded to the type for the product with V; they are taken against a
+// reference exponent that trails the row's maximum: REF_SHIFT below it when it is set, raised when a score exceeds it by more than
+// SLACK.  bf16 has the exponent range for large slack (rare raises); f16 ends at 2^16, and starts to lose bits at 2^-14:
+// the shift keeps what is 2^-22 of the largest at full precision.
+template <typename T> struct Elem;
+template <> struct Elem<__bf16> {
+  typedef __bf16 x8 __attribute__((ext_vector_type(8)));
+  static constexpr float SLACK = 40.f, SHIFT = 0.f;
+  static __device__ __forceinline__ floatx4 mfma(x8 a, x8 b, floatx4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+  static constexpr unsigned INF = 0x7f80u;
+};
+template <> struct Elem<_Float16> {
+  typedef _Float16 x8 __attribute__((ext_vector_type(8)));
+  static constexpr float SLACK = 15.f, SHIFT = 8.f;
+  static __device__ __forceinline__ floatx4 mfma(x8 a, x8 b, floatx4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
+  static constexpr unsigned INF = 0x7c00u;
+};
+
+struct PagedAttnArgs {
+  PagedArgs c;
+  const void *k_pages, *v_pages, *q;
+  long long q_tok, q_head, o_tok, o_head;      // elements
+  void* out;
+  float* lse;
+  const uint64_t* anc;
+  int n_rows, Hq, Hkv;
+  FastDiv group, heads;                        // query heads per KV head; KV heads
+  float scale_log2;                            // scale * log2(e): scores are kept in the log2 domain
+  int page_run;                                // pages are whole multiples of this many tokens (8, or 1)
+  int splits;                                  // whether units may be split
+  float* part_o;                               // [grid][rows per block][D]
+  float* part_ml;                              // [grid][rows per block][2]
+  int2* row_parts;                             // [n_rows*Hq] first partial row, how many parts
+  long long part_rows;                         // rows of part_o
+  int block_rows;
+  int32_t* fault;
+};
+
+struct Seq { int first, n, ctx; bool good; };
+__device__ __forceinline__ Seq sequence(const PagedAttnArgs& a, int s) {
+  Seq q;
+  q.first = a.c.q_off[s]; q.ctx = a.c.ctx_len[s];
+  const int next = a.c.q_off[s + 1];
+  const bool rows = q.first >= 0 && next <= a.n_rows && next > q.first;
+  q.n = rows ? next - q.first : 0;
+  q.good = rows && q.n <= a.c.max_new && q.ctx >= 0 && q.ctx <= a.c.max_len - q.n && !(a.anc && q.n > 64);
+  if (!q.good) q.ctx = 0;
+  return q;
+}
+
+struct Unit { int s, g, rb, part, nparts; };
+
+// Which unit, and which part of it, a workgroup has: lengths lie in device memory, so every wave works it out for itself, a
+// lane per sequence (64 at a time).  A part is `len` steps long, the same for all: an even share of all units' steps over
+// the workgroups that the device holds.  False: nothing to do.
+template <int STEP>
+__device__ __forceinline__ bool find_unit(const PagedAttnArgs& a, int slots, Unit& u, int& part_steps) {
+  const int lane = threadIdx.x & 63, rows = a.block_rows;
+  const int at = quotient(a.heads, blockIdx.x);
+  u.g = blockIdx.x - at * a.Hkv;
+  auto measure = [&](int s, int& nrb, int& steps) {
+    nrb = 0; steps = 0;
+    if (s < a.c.n_seqs) {
+      const Seq q = sequence(a, s);
+      nrb = (int)(((long long)q.n * a.group.d + rows - 1) / rows);
+      steps = q.good ? (q.ctx + q.n + STEP - 1) / STEP : 1;
+    }
+  };
+  int len = 0x7fffffff;
+  if (a.splits) {
+    double total = 0.0;
+    for (int s0 = 0; s0 < a.c.n_seqs; s0 += 64) {
+      int nrb, steps;
+      measure(s0 + lane, nrb, steps);
+      total += (double)nrb * (double)steps;
+    }
+    total = wave_sum(total) * a.Hkv;
+    len = (int)fmin(ceil(total / slots), 1e9);
+    len = max(len, PA_MIN_STEPS);
+  }
+  part_steps = len;
+  long long base = 0;
+  for (int s0 = 0; s0 < a.c.n_seqs; s0 += 64) {
+    int nrb, steps;
+    measure(s0 + lane, nrb, steps);
+    const int np = steps > len ? (steps + len - 1) / len : 1;
+    int upto = nrb * np;                       // inclusive sum over the lanes
+    const int mine = upto;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) { const int o = __shfl_up(upto, d); if (lane >= d) upto += o; }
+    const long long begin = base + upto - mine;
+    const unsigned long long m = __ballot(at >= begin && at < begin + mine);
+    if (m) {
+      const int l = (int)__ffsll((long long)m) - 1;
+      u.s = s0 + l;
+      u.nparts = __builtin_amdgcn_readlane(np, l);
+      const int rel = at - (int)__builtin_amdgcn_readlane((int)begin, l);
+      const int n = __builtin_amdgcn_readlane(nrb, l), block = rel / u.nparts;
+      u.part = rel - block * u.nparts;
+      u.rb = n - 1 - block;                    // blocks that see most first
+      return true;
+    }
+    base += __builtin_amdgcn_readlane(upto, 63);
+  }
+  return false;
+}
+
+// Bits of the tokens tok0 .. tok0+31 that a row sees: those in front of `limit`, or the context and its mask's bits.
+__device__ __forceinline__ uint32_t seen_bits(const PagedAttnArgs& a, int tok0, int limit, int ctx, uint64_t anc) {
+  if (!a.anc) {
+    const int n = limit - tok0;
+    return n >= 32 ? 0xffffffffu : n <= 0 ? 0u : (1u << n) - 1;
+  }
+  const int j = tok0 - ctx;
+  if (j >= 64) return 0u;
+  if (j >= 0) return (uint32_t)(anc >> j);
+  if (j <= -32) return 0xffffffffu;
+  return (uint32_t)(anc << -j) | ((1u << -j) - 1);
+}
+
+template <typename T>
+__device__ __forceinline__ bool any_nonfinite(uint4 w) {
+  const unsigned e = Elem<T>::INF, m = e | (e << 16);
+  auto one = [&](unsigned x) { x &= m; return (x & 0xffffu) == e || (x >> 16) == e; };
+  return one(w.x) | one(w.y) | one(w.z) | one(w.w);
+}
+__device__ __forceinline__ uint4 load16(const void* p) {
+  const u32x4 v = __builtin_nontemporal_load((const gvec*)p);
+  return make_uint4(v.x, v.y, v.z, v.w);
+}
+// The wave's own LDS traffic so far is done.
+__device__ __forceinline__ void wave_lds_fence() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+
+// Four channels of a finished row, and once per row the log-sum-exp.
+template <typename T, int D>
+__device__ __forceinline__ void write_row(const PagedAttnArgs& a, long long row, int head, int part, float M, float L, floatx4 acc) {
+  const float inv = L > 0.f || L != L ? 1.f / L : 0.f;
+  union { T h[4]; uint2 u; } pk;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) pk.h[i] = (T)(L > 0.f || L != L ? acc[i] * inv : 0.f);
+  *reinterpret_cast<uint2*>(static_cast<T*>(a.out) + row * a.o_tok + head * a.o_head + 4 * part) = pk.u;
+  if (a.lse && part == 0) a.lse[row * a.Hq + head] = L > 0.f || L != L ? (M + log2f(L)) * 0.6931471805599453f : -INFINITY;
+}
+
+template <typename T, int D, int NRT>
+__global__ __launch_bounds__(PA_BLOCK) void paged_wave_kernel(PagedAttnArgs a) {
+  typedef typename Elem<T>::x8 x8;
+  constexpr int TW = PA_BLOCK / 64;
+  constexpr int DS = D / 32, DT = D / 16, ROWS = 16 * NRT;
+  constexpr int LPR = D / 8, TG = 64 / LPR, ROUNDS = PA_STEP / TG;
+  constexpr int KP = D + 8, OP = D + 4;
+  static_assert(ROWS * OP * 4 <= 2 * PA_STEP * KP * 2, "a wave's partial output takes the place of its tiles");
+  static_assert(ROWS * (PA_STEP + 1) * 4 <= PA_STEP * KP * 2, "numerators in the place of the K tile");
+  __shared__ __attribute__((aligned(16))) T tiles[TW][2 * PA_STEP * KP];
+  __shared__ float wave_ml[TW][ROWS][2];
+
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = lane & 15, qd = lane >> 4;
+  Unit u;
+  int part_steps;
+  if (!find_unit<PA_STEP>(a, PA_SLOTS, u, part_steps)) return;
+  const Seq sq = sequence(a, u.s);
+  const int R = sq.n * a.group.d, row0 = u.rb * ROWS;
+  const int len = sq.ctx + sq.n;
+  const bool reporter = u.g == 0 && u.rb == 0 && u.part == 0 && threadIdx.x == 0;
+  if (reporter && !sq.good) atomicOr(a.fault, DSBD_FAULT_BOUNDS);
+  // tokens that the block's last row sees, and the part's steps
+  const int last_tok = quotient(a.group, min(row0 + ROWS, R) - 1), first_tok = quotient(a.group, row0);
+  const int upto = !sq.good ? 0 : a.anc ? len : sq.ctx + last_tok + 1;
+  const int steps = (upto + PA_STEP - 1) / PA_STEP;
+  const int st_begin = u.nparts == 1 ? 0 : (int)min((long long)u.part * part_steps, (long long)steps);
+  const int st_end = u.nparts == 1 ? steps : min(steps, st_begin + part_steps);
+
+  // ---- query rows
+  x8 qf[NRT][DS];
+  int limit[NRT];
+  uint64_t anc[NRT];
+#pragma unroll
+  for (int rt = 0; rt < NRT; ++rt) {
+    const int r = row0 + 16 * rt + col;
+    const bool live = r < R;
+    const int tok = quotient(a.group, live ? r : row0), head = u.g * a.group.d + (live ? r - tok * a.group.d : 0);
+    limit[rt] = live ? sq.ctx + tok + 1 : 0;
+    anc[rt] = live && a.anc ? a.anc[sq.first + tok] : 0ull;
+    const T* qp = static_cast<const T*>(a.q) + (long long)(sq.first + tok) * a.q_tok + head * a.q_head + 8 * qd;
+#pragma unroll
+    for (int j = 0; j < DS; ++j) {
+      union { u32x4 u; x8 v; } c;
+      c.u = u32x4{0, 0, 0, 0};
+      if (live) c.u = *(const gvec*)(qp + 32 * j);
+      qf[rt][j] = c.v;
+    }
+  }
+  floatx4 o[NRT][DT];
+  float m_ref[NRT], l_run[NRT];
+#pragma unroll
+  for (int rt = 0; rt < NRT; ++rt) {
+    m_ref[rt] = -INFINITY; l_run[rt] = 0.f;
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt) o[rt][dt] = floatx4{0.f, 0.f, 0.f, 0.f};
+  }
+
+  T* const kt = tiles[wave];
+  T* const vt = kt + PA_STEP * KP;
+  const int piece = lane % LPR, ld_tok = ROUNDS * (lane / LPR);    // this lane loads tokens ld_tok .. ld_tok+ROUNDS-1 of a step
+  const long long hoff = (long long)u.g * a.c.head_stride + 8 * piece;
+  const T* const kp = static_cast<const T*>(a.k_pages) + hoff;
+  const T* const vp = static_cast<const T*>(a.v_pages) + hoff;
+  const int32_t* const table = a.c.page_table + (long long)u.s * a.c.table_stride;
+  uint4 kr[ROUNDS], vr[ROUNDS];
+  unsigned ok;                      // bit k: the lane's token k is there
+  auto load_step = [&](int st) {
+    const int t0 = st * PA_STEP + ld_tok;
+    ok = 0;
+    long long off = 0;
+    bool there = false;
+#pragma unroll
+    for (int k = 0; k < ROUNDS; ++k) {
+      const int t = t0 + k;
+      if (k == 0 || a.page_run < ROUNDS) {
+        const int p = quotient(a.c.page, min(t, len - 1));
+        const int page = p < a.c.table_stride ? table[p] : -1;
+        there = page >= 0 && page < a.c.n_pages;
+        off = there ? (long long)page * a.c.page_stride + (long long)(min(t, len - 1) - p * a.c.page.d) * a.c.token_stride : 0;
+        if (!there && t < len) atomicOr(a.fault, DSBD_FAULT_BOUNDS);
+      } else off += t < len ? a.c.token_stride : 0;
+      kr[k] = vr[k] = make_uint4(0, 0, 0, 0);
+      if (there && t < len) { kr[k] = load16(kp + off); vr[k] = load16(vp + off); ok |= 1u << k; }
+    }
+  };
+  int st = st_begin + wave;
+  if (st < st_end) load_step(st);
+  const int open = sq.ctx + (a.anc ? 0 : first_tok + 1);      // tokens in front of this are seen by all rows
+  for (; st < st_end; st += TW) {
+    const int tok0 = st * PA_STEP;
+    uint32_t valid = 0xffffffffu;
+    const bool whole = __all(ok == (1u << ROUNDS) - 1);
+    if (!whole) {
+      valid = 0;
+#pragma unroll
+      for (int k = 0; k < TG; ++k) valid |= (uint32_t)__builtin_amdgcn_readlane((int)ok, k * LPR) << (ROUNDS * k);
+    }
+    const bool masked = !whole || tok0 + PA_STEP > open;
+    bool odd = false;                // values that no product with 0 makes 0
+    if (masked) {
+#pragma unroll
+      for (int k = 0; k < ROUNDS; ++k) odd |= any_nonfinite<T>(vr[k]);
+      odd = __any(odd);
+    }
+    wave_lds_fence();
+#pragma unroll
+    for (int k = 0; k < ROUNDS; ++k) {
+      *reinterpret_cast<uint4*>(&kt[(ld_tok + k) * KP + 8 * piece]) = kr[k];
+      *reinterpret_cast<uint4*>(&vt[(ld_tok + k) * KP + 8 * piece]) = vr[k];
+    }
+    wave_lds_fence();
+    if (st + TW < st_end) load_step(st + TW);
+    floatx4 s[NRT][2];
+#pragma unroll
+    for (int tt = 0; tt < 2; ++tt) {
+      x8 kf[DS];
+#pragma unroll
+      for (int j = 0; j < DS; ++j) kf[j] = *reinterpret_cast<const x8*>(&kt[(16 * tt + col) * KP + 32 * j + 8 * qd]);
+#pragma unroll
+      for (int rt = 0; rt < NRT; ++rt) {
+        floatx4 acc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int j = 0; j < DS; ++j) acc = Elem<T>::mfma(kf[j], qf[rt][j], acc);
+        s[rt][tt] = acc * a.scale_log2;
+      }
+    }
+    if (masked) {
+#pragma unroll
+      for (int rt = 0; rt < NRT; ++rt) {
+        const uint32_t b = valid & (limit[rt] ? seen_bits(a, tok0, limit[rt], sq.ctx, anc[rt]) : 0u);
+#pragma unroll
+        for (int tt = 0; tt < 2; ++tt)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) if (!((b >> (16 * tt + 4 * qd + i)) & 1)) s[rt][tt][i] = -INFINITY;
+      }
+    }
+    x8 pf[NRT];
+#pragma unroll
+    for (int rt = 0; rt < NRT; ++rt) {
+      float mx = s[rt][0][0];
+#pragma unroll
+      for (int k = 1; k < 8; ++k) mx = fmaxf(mx, s[rt][k >> 2][k & 3]);
+      if (__any(mx > m_ref[rt] + Elem<T>::SLACK)) {
+        mx = fmaxf(mx, __shfl_xor(mx, 16));
+        mx = fmaxf(mx, __shfl_xor(mx, 32));
+        if (mx > m_ref[rt] + Elem<T>::SLACK) {
+          const float to = mx - Elem<T>::SHIFT;
+          const float f = m_ref[rt] == -INFINITY ? 0.f : exp2f(m_ref[rt] - to);
+          m_ref[rt] = to;
+          l_run[rt] *= f;
+#pragma unroll
+          for (int dt = 0; dt < DT; ++dt) o[rt][dt] *= f;
+        }
+      }
+      const float ref = m_ref[rt] == -INFINITY ? 0.f : m_ref[rt];
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        const float p = __builtin_amdgcn_exp2f(s[rt][k >> 2][k & 3] - ref);
+        s[rt][k >> 2][k & 3] = p;
+        l_run[rt] += p;
+        pf[rt][k] = (T)p;
+      }
+    }
+    if (!odd) {
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt) {
+        union { v4i16 h[2]; x8 v; } vf;
+        const T* rowp = &vt[(4 * qd + (col >> 2)) * KP + 16 * dt + 4 * (col & 3)];
+        vf.h[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4i16*)(rowp));
+        vf.h[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4i16*)(rowp + 16 * KP));
+#pragma unroll
+        for (int rt = 0; rt < NRT; ++rt) o[rt][dt] = Elem<T>::mfma(vf.v, pf[rt], o[rt][dt]);
+      }
+    } else {
+      // NaN or Inf among the values of a step that not all rows see whole: token by token, so that a row only takes what it
+      // sees (a product with a numerator of 0 would be NaN)
+      float* const pb = reinterpret_cast<float*>(kt);
+      wave_lds_fence();
+#pragma unroll
+      for (int rt = 0; rt < NRT; ++rt)
+#pragma unroll
+        for (int k = 0; k < 8; ++k) pb[(16 * rt + col) * (PA_STEP + 1) + 16 * (k >> 2) + 4 * qd + (k & 3)] = (float)pf[rt][k];
+      wave_lds_fence();
+      for (int t = 0; t < PA_STEP; ++t) {
+#pragma unroll
+        for (int rt = 0; rt < NRT; ++rt) {
+          const float p = pb[(16 * rt + col) * (PA_STEP + 1) + t];
+#pragma unroll
+          for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) o[rt][dt][i] += p != 0.f ? p * (float)vt[t * KP + 16 * dt + 4 * qd + i] : 0.f;
+        }
+      }
+    }
+  }
+  // ---- the waves' results: sums over the lanes of a row, then everything through the LDS
+#pragma unroll
+  for (int rt = 0; rt < NRT; ++rt) {
+    l_run[rt] += __shfl_xor(l_run[rt], 16);
+    l_run[rt] += __shfl_xor(l_run[rt], 32);
+  }
+  float* const po = reinterpret_cast<float*>(tiles[wave]);
+  wave_lds_fence();
+#pragma unroll
+  for (int rt = 0; rt < NRT; ++rt) {
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt) *reinterpret_cast<floatx4*>(&po[(16 * rt + col) * OP + 16 * dt + 4 * qd]) = o[rt][dt];
+    if (qd == 0) { wave_ml[wave][16 * rt + col][0] = m_ref[rt]; wave_ml[wave][16 * rt + col][1] = l_run[rt]; }
+  }
+  __syncthreads();
+  const long long slot = (long long)blockIdx.x * ROWS;
+  for (int i = threadIdx.x; i < ROWS * (D / 4); i += PA_BLOCK) {
+    const int rl = i / (D / 4), part = i % (D / 4), r = row0 + rl;
+    if (r >= R) continue;
+    float M = -INFINITY, L = 0.f;
+#pragma unroll
+    for (int w = 0; w < TW; ++w) M = fmaxf(M, wave_ml[w][rl][0]);
+    floatx4 acc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int w = 0; w < TW; ++w) {
+      const float m = wave_ml[w][rl][0], l = wave_ml[w][rl][1];
+      if (l == 0.f) continue;                    // the wave's steps had nothing for this row
+      const float f = m == M ? 1.f : exp2f(m - M);
+      L += l * f;
+      acc += *reinterpret_cast<const floatx4*>(&reinterpret_cast<const float*>(tiles[w])[rl * OP + 4 * part]) * f;
+    }
+    const int tok = quotient(a.group, r), head = u.g * a.group.d + r - tok * a.group.d;
+    const long long row = sq.first + tok;
+    if (u.nparts == 1) {
+      write_row<T, D>(a, row, head, part, M, L, acc);
+    } else {
+      *reinterpret_cast<floatx4*>(&a.part_o[(slot + rl) * D + 4 * part]) = acc;
+      if (part == 0) { a.part_ml[2 * (slot + rl)] = M; a.part_ml[2 * (slot + rl) + 1] = L; }
+    }
+    if (a.splits && part == 0 && u.part == 0) a.row_parts[row * a.Hq + head] = make_int2((int)blockIdx.x * ROWS + rl, u.nparts);
+  }
+}
+
+// A wave per (row, head) of what was split: the parts of a unit are Hkv * rows apart.
+template <typename T, int D>
+__global__ __launch_bounds__(PA_BLOCK) void paged_join_kernel(PagedAttnArgs a) {
+  const long long id = (long long)blockIdx.x * (PA_BLOCK / 64) + (threadIdx.x >> 6);
+  const int lane = threadIdx.x & 63;
+  if (id >= (long long)a.n_rows * a.Hq) return;
+  const int row = (int)(id / a.Hq), head = (int)(id % a.Hq);
+  if (row < a.c.q_off[0] || row >= a.c.q_off[a.c.n_seqs]) return;       // padding
+  const int2 rp = a.row_parts[id];
+  const long long apart = (long long)a.Hkv * a.block_rows;
+  if (rp.y <= 1 || rp.x < 0 || rp.x + (rp.y - 1) * apart >= a.part_rows) return;
+  constexpr int PIECES = D / 4, GROUPS = 64 / PIECES;                   // groups of lanes take every GROUPS-th part
+  const int part = lane % PIECES, grp = lane / PIECES;
+  float M = -INFINITY;
+  for (int k = lane; k < rp.y; k += 64) M = fmaxf(M, a.part_ml[2 * (rp.x + k * apart)]);
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) M = fmaxf(M, __shfl_xor(M, d));
+  floatx4 acc = {0.f, 0.f, 0.f, 0.f};
+  float L = 0.f;
+#pragma unroll 4
+  for (int k = grp; k < rp.y; k += GROUPS) {
+    const long long at = rp.x + k * apart;
+    const float m = a.part_ml[2 * at], l = a.part_ml[2 * at + 1];
+    if (l == 0.f) continue;
+    const float f = m == M ? 1.f : exp2f(m - M);
+    L += l * f;
+    acc += *reinterpret_cast<const floatx4*>(&a.part_o[at * D + 4 * part]) * f;
+  }
+#pragma unroll
+  for (int d = PIECES; d < 64; d <<= 1) {
+    L += __shfl_xor(L, d);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) acc[i] += __shfl_xor(acc[i], d);
+  }
+  if (grp == 0) write_row<T, D>(a, row, head, part, M, L, acc);
+}
+
+// How a call is cut up.
+struct Plan {
+  int rows;                  // per block
+  long long grid;
+  bool splits;
+  size_t bytes;
+};
+Plan plan(const dsbd_paged_kv* c, int n_rows, int Hq, int Hkv, int D, PagedAttnArgs* a, void* workspace) {
+  Plan p;
+  const long long group = Hq / Hkv;
+  p.rows = (long long)c->max_new * group <= 16 ? 16 : 32;
+  const long long units = ((long long)n_rows * group / p.rows + c->n_seqs) * Hkv;      // at most
+  p.splits = units < 2 * PA_SLOTS;
+  p.grid = units + (p.splits ? PA_SLOTS : 0);
+  WorkspaceCarver w(workspace);
+  float *po = nullptr, *ml = nullptr;
+  int2* rp = nullptr;
+  if (p.splits) {
+    rp = w.take<int2>((size_t)n_rows * Hq);
+    ml = w.take<float>((size_t)p.grid * p.rows * 2);
+    po = w.take<float>((size_t)p.grid * p.rows * D);
+  }
+  p.bytes = std::max<size_t>(w.total(), 256);
+  if (a) {
+    a->splits = p.splits; a->part_o = po; a->part_ml = ml; a->row_parts = rp;
+    a->part_rows = p.grid * p.rows; a->block_rows = p.rows;
+  }
+  return p;
+}
+
+int32_t check(const dsbd_paged_kv* cache, int32_t n_rows, int32_t Hq, int32_t Hkv, int32_t D) {
+  if (!cache) return DSBD_ERR_INVALID;
+  if (Hq < 1 || Hkv < 1 || Hq % Hkv) return DSBD_ERR_INVALID;
+  if (D != 64 && D != 128) return DSBD_ERR_UNSUPPORTED;
+  if (Hq > 65535 || (long long)n_rows * Hq > (1ll << 30)) return DSBD_ERR_UNSUPPORTED;
+  return DSBD_OK;
+}
+
+}  // namespace
+
+extern "C" size_t dsbd_paged_attention_workspace_bytes(const dsbd_paged_kv* cache, int32_t n_rows, int32_t Hq, int32_t Hkv, int32_t D) {
+  if (check(cache, n_rows, Hq, Hkv, D) != DSBD_OK || n_rows < 0 || cache->n_seqs < 0 || cache->max_new < 0) return 0;
+  return plan(cache, n_rows, Hq, Hkv, D, nullptr, nullptr).bytes;
+}
+
+extern "C" int32_t dsbd_paged_attention(const dsbd_paged_kv* cache, int32_t n_rows, int32_t Hq, int32_t Hkv, int32_t D, int32_t dtype,
+                                        const dsbd_rows* q, float scale, const uint64_t* anc_mask, const dsbd_rows* out, float* lse,
+                                        void* workspace, size_t workspace_bytes, int32_t* fault, void* stream_) {
+  int32_t rc = check(cache, n_rows, Hq, Hkv, D);
+  if (rc != DSBD_OK) return rc;
+  if (dtype != DSBD_BF16 && dtype != DSBD_F16) return DSBD_ERR_UNSUPPORTED;
+  rc = paged_check(cache, n_rows, Hkv);
+  if (rc != DSBD_OK) return rc;
+  if (anc_mask && cache->max_new > 64) return DSBD_ERR_UNSUPPORTED;
+  if (n_rows == 0 || cache->n_seqs == 0) return DSBD_OK;
+  if (!q || !out || !q->ptr || !out->ptr || !fault || !workspace) return DSBD_ERR_INVALID;
+  if ((reinterpret_cast<uintptr_t>(q->ptr) | reinterpret_cast<uintptr_t>(out->ptr)) & 15) return DSBD_ERR_INVALID;
+  if (q->token_stride < 0 || q->head_stride < 0 || out->token_stride < 0 || out->head_stride < 0) return DSBD_ERR_INVALID;
+  if ((q->token_stride | q->head_stride | out->token_stride | out->head_stride) & 7) return DSBD_ERR_UNSUPPORTED;
+  if (reinterpret_cast<uintptr_t>(workspace) & 255) return DSBD_ERR_INVALID;
+  PagedAttnArgs a;
+  const Plan p = plan(cache, n_rows, Hq, Hkv, D, &a, workspace);
+  if (workspace_bytes < p.bytes) return DSBD_ERR_WORKSPACE;
+  if (p.grid > 0x7fffffffLL / p.rows) return DSBD_ERR_UNSUPPORTED;
+  a.c = paged_args(cache);
+  a.k_pages = cache->k_pages; a.v_pages = cache->v_pages; a.q = q->ptr; a.out = out->ptr; a.lse = lse; a.anc = anc_mask;
+  a.q_tok = q->token_stride; a.q_head = q->head_stride; a.o_tok = out->token_stride; a.o_head = out->head_stride;
+  a.n_rows = n_rows; a.Hq = Hq; a.Hkv = Hkv; a.group = fast_div(Hq / Hkv); a.heads = fast_div(Hkv);
+  a.scale_log2 = (float)((scale > 0.f ? (double)scale : 1.0 / sqrt((double)D)) * 1.4426950408889634);
+  a.page_run = cache->page_size % 8 == 0 ? 8 : 1;
+  a.fault = fault;
+  hipStream_t stream = static_cast<hipStream_t>(stream_);
+  const dim3 grid((unsigned)p.grid), block(PA_BLOCK);
+  const dim3 join((unsigned)(((long long)n_rows * Hq + PA_BLOCK / 64 - 1) / (PA_BLOCK / 64)));
+#define PA_ROWS(T, DD)                                                                                     \
+  do {                                                                                                     \
+    if (p.rows == 16) hipLaunchKernelGGL((paged_wave_kernel<T, DD, 1>), grid, block, 0, stream, a);        \
+    else hipLaunchKernelGGL((paged_wave_kernel<T, DD, 2>), grid, block, 0, stream, a);                     \
+    DSBD_HIP_LAUNCH_CHECK();                                                                               \
+    if (p.splits) hipLaunchKernelGGL((paged_join_kernel<T, DD>), join, block, 0, stream, a);               \
+  } while (0)
+#define PA_TYPES(DD) do { if (dtype == DSBD_BF16) PA_ROWS(__bf16, DD); else PA_ROWS(_Float16, DD); } while (0)
+  if (D == 128) PA_TYPES(128);
+  else PA_TYPES(64);
+#undef PA_TYPES
+#undef PA_ROWS
+  DSBD_HIP_LAUNCH_CHECK();
+  return DSBD_OK;
+}
