@@ -489,13 +489,13 @@ typedef struct dsbd_logit_rules {
   /* The text of a beam: its tokens in front of the tree's root, then the nodes of the row's path (root first, the row's
    * node last).  The first prompt_len tokens of the text are the prompt, the others were generated. */
   const int32_t*  hist;          /* [n_hist]                                                                  */
-  const int32_t*  hist_off;      /* [n_trees+1] ascending: tokens in front of tree b's root                   */
+  const int32_t*  hist_off;      /* [n_trees+1] ascending: tokens in front of tree b's root (< 2^24 of them)  */
   const int32_t*  prompt_len;    /* [n_trees]; NULL: 0                                                        */
   /* [n_prompts] each */
-  const float*    repetition;    /* > 0: a token of the text: z > 0 ? z / r : z * r                           */
+  const float*    repetition;    /* > 0 (a normal number): a token of the text: z > 0 ? z / r : z * r         */
   const float*    frequency;     /* z -= frequency * (times the token was generated)                          */
   const float*    presence;      /* z -= presence, if it was generated                                        */
-  const float*    temperature;   /* > 0: z /= temperature, behind the biases                                  */
+  const float*    temperature;   /* > 0 (a normal number): z /= temperature, behind the biases                */
   /* biases: prompt p adds bias_value[i] to token bias_token[i], i in bias_off[p] .. bias_off[p+1]-1; of several entries
    * for one token the last counts */
   const int32_t*  bias_off;      /* [n_prompts+1] ascending, within [0, n_bias]                               */
@@ -514,9 +514,10 @@ typedef struct dsbd_logit_rules {
  * Row i belongs to node i, or to node row_node[i] (the nodes of one layer, as dsbd_build_forest lists them); forest->token
  * is needed.  logits [n_rows,V] of type DSBD_F32, DSBD_BF16 or DSBD_F16, rows logits_stride elements apart; out [n_rows,V]
  * f32, rows out_stride apart, may be `logits` itself (f32, same stride).
- * Device-side problems: trees as in dsbd_forest_attention, a row_node outside the forest (DSBD_FAULT_TOPOLOGY: the row
- * is copied), token ids outside [0, V) (DSBD_FAULT_TOKEN: ignored), offsets or a mask_row outside their arrays, a
- * repetition or temperature that is not above 0 (DSBD_FAULT_BOUNDS: that rule is left out).
+ * Device-side problems: trees as in dsbd_forest_attention (the rows of a tree with unusable offsets, and of nodes behind a
+ * tree's max_tree_nodes, are not written), a row_node outside the trees (DSBD_FAULT_TOPOLOGY: the row is copied), token ids outside
+ * [0, V) (DSBD_FAULT_TOKEN: ignored), offsets or a mask_row outside their arrays, a repetition or temperature that is not
+ * above 0 (DSBD_FAULT_BOUNDS: that rule is left out).
  */
 int32_t dsbd_process_logits(const dsbd_forest* forest, const int32_t* row_node, int32_t n_rows, int32_t V, int32_t dtype,
                             const void* logits, int64_t logits_stride, const dsbd_logit_rules* rules, float* out,
