@@ -19,8 +19,10 @@ namespace {
 #define PA_STEP 32                 // tokens per wave step
 #define PA_SLOTS 512               // workgroups of the wave-private kernel that the device holds (70 KB of LDS each)
 #define PA_MIN_STEPS 4             // steps that a part has at least
+#define PA_TILE_SLOTS 512           // workgroups of the tile kernel that the device holds
 
 typedef float floatx4 __attribute__((ext_vector_type(4)));
+typedef float floatx16 __attribute__((ext_vector_type(16)));
 typedef short v4i16 __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) v4i16 lds_v4i16;
 typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
@@ -35,12 +37,14 @@ template <> struct Elem<__bf16> {
   typedef __bf16 x8 __attribute__((ext_vector_type(8)));
   static constexpr float SLACK = 40.f, SHIFT = 0.f;
   static __device__ __forceinline__ floatx4 mfma(x8 a, x8 b, floatx4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+  static __device__ __forceinline__ floatx16 mfma(x8 a, x8 b, floatx16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
   static constexpr unsigned INF = 0x7f80u;
 };
 template <> struct Elem<_Float16> {
   typedef _Float16 x8 __attribute__((ext_vector_type(8)));
   static constexpr float SLACK = 15.f, SHIFT = 8.f;
   static __device__ __forceinline__ floatx4 mfma(x8 a, x8 b, floatx4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
+  static __device__ __forceinline__ floatx16 mfma(x8 a, x8 b, floatx16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
   static constexpr unsigned INF = 0x7c00u;
 };
 
@@ -163,15 +167,22 @@ __device__ __forceinline__ void wave_lds_fence() {
   __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
 }
 
-// Four channels of a finished row, and once per row the log-sum-exp.
+// Four channels of a finished row, and once per row the log-sum-exp.  `lost`: two bits per channel whose sum is +Inf, -Inf, NaN.
 template <typename T, int D>
-__device__ __forceinline__ void write_row(const PagedAttnArgs& a, long long row, int head, int part, float M, float L, floatx4 acc) {
-  const float inv = L > 0.f || L != L ? 1.f / L : 0.f;
-  union { T h[4]; uint2 u; } pk;
+__device__ __forceinline__ void write_row(const PagedAttnArgs& a, long long row, int head, int part, float M, float L, floatx4 acc, unsigned lost = 0) {
+  const float inv = L != 0.f ? 1.f / L : 0.f;
+  union { T h[4]; unsigned short b[4]; uint2 u; } pk;
 #pragma unroll
-  for (int i = 0; i < 4; ++i) pk.h[i] = (T)(L > 0.f || L != L ? acc[i] * inv : 0.f);
+  for (int i = 0; i < 4; ++i) pk.h[i] = (T)(L != 0.f ? acc[i] * inv : 0.f);
+  if (lost) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const unsigned k = (lost >> (2 * i)) & 3;
+      if (k) pk.b[i] = (unsigned short)(Elem<T>::INF | (k == 2 ? 0x8000u : k == 3 ? 0x40u | (Elem<T>::INF >> 1) : 0u));
+    }
+  }
   *reinterpret_cast<uint2*>(static_cast<T*>(a.out) + row * a.o_tok + head * a.o_head + 4 * part) = pk.u;
-  if (a.lse && part == 0) a.lse[row * a.Hq + head] = L > 0.f || L != L ? (M + log2f(L)) * 0.6931471805599453f : -INFINITY;
+  if (a.lse && part == 0) a.lse[row * a.Hq + head] = L != 0.f ? (M + log2f(L)) * 0.6931471805599453f : -INFINITY;
 }
 
 template <typename T, int D, int NRT>
@@ -412,6 +423,295 @@ __global__ __launch_bounds__(PA_BLOCK) void paged_wave_kernel(PagedAttnArgs a) {
   }
 }
 
+// ---- tile kernel: many rows on the same keys
+//
+// Four waves of 32 * RT rows each share tiles of 64 tokens of K and V in the LDS, two of each, filled by direct loads (no
+// registers in between) a tile ahead; the pieces of a row are swizzled by the token, so that the operand reads, which go down the
+// rows, spread over the banks.  MFMA 32x32x16: S^T = K Q^T and O^T += V^T P^T as in the wave-private kernel, a lane owns a query
+// row together with the lane 32 further on, which has the other half of its tokens.
+#define PA_TILE 64
+
+typedef __attribute__((address_space(3))) void lds_void;
+typedef const __attribute__((address_space(1))) void glb_cvoid;
+
+// Workgroup barrier that orders LDS traffic only (loads in flight stay in flight).
+__device__ __forceinline__ void lds_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+
+template <typename T, int D, int RT>
+__global__ __launch_bounds__(PA_BLOCK, RT == 1 ? 2 : 1) void paged_tile_kernel(PagedAttnArgs a) {
+  typedef typename Elem<T>::x8 x8;
+  constexpr int DS = D / 16, DT = D / 32;               // k-steps of S^T, channel tiles of O^T
+  constexpr int ROWS_W = 32 * RT, ROWS = 4 * ROWS_W;
+  constexpr int PPR = D / 8, ROWB = 2 * D;              // 16-byte pieces and bytes of a row
+  constexpr int TPI = 64 / PPR, ROUNDS = PA_TILE / (4 * TPI);     // tokens per load instruction, instructions per wave and tile
+  __shared__ uint4 kA[PA_TILE * PPR], kB[PA_TILE * PPR], vA[PA_TILE * PPR], vB[PA_TILE * PPR];
+  // two bits per row and channel whose sum is +Inf, -Inf or NaN (both)
+  __shared__ unsigned lost[ROWS][D / 16];
+  __shared__ int any_lost;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 31, h = lane >> 5;
+  Unit u;
+  int part_tiles;
+  if (!find_unit<PA_TILE>(a, PA_TILE_SLOTS, u, part_tiles)) return;
+  const Seq sq = sequence(a, u.s);
+  const int R = sq.n * a.group.d, row0 = u.rb * ROWS, len = sq.ctx + sq.n;
+  if (u.g == 0 && u.rb == 0 && u.part == 0 && threadIdx.x == 0 && !sq.good) atomicOr(a.fault, DSBD_FAULT_BOUNDS);
+  const int last_tok = quotient(a.group, min(row0 + ROWS, R) - 1), first_tok = quotient(a.group, row0);
+  const int upto = !sq.good ? 0 : a.anc ? len : sq.ctx + last_tok + 1;
+  const int tiles = (upto + PA_TILE - 1) / PA_TILE;
+  const int t_begin = u.nparts == 1 ? 0 : (int)min((long long)u.part * part_tiles, (long long)tiles);
+  const int t_end = u.nparts == 1 ? tiles : min(tiles, t_begin + part_tiles);
+  const int open = sq.ctx + (a.anc ? 0 : first_tok + 1);      // tokens in front of this are seen by all rows
+
+  // ---- where tokens lie: lane l looks up token l of a tile; invalid ones read the first query row instead, and are masked
+  const int32_t* const table = a.c.page_table + (long long)u.s * a.c.table_stride;
+  auto look_up = [&](int ti) { const int t = min(ti * PA_TILE + lane, len - 1), p = quotient(a.c.page, t);
+    return p < a.c.table_stride ? table[p] : -1; };
+  // swizzles: K is read down 16 tokens at one piece, V down 8 tokens at 4 pieces in a row
+  auto swz_k = [](int t) { return D == 128 ? t & 15 : (t >> 1) & 7; };
+  auto swz_v = [](int t) { return D == 128 ? 4 * (t & 3) : 4 * ((t >> 1) & 1); };
+  const int ld_tok = TPI * wave + lane / PPR, ld_k = (lane % PPR) ^ swz_k(ld_tok), ld_v = (lane % PPR) ^ swz_v(ld_tok);
+  static_assert((4 * TPI) % 16 == 0, "a round is a whole number of swizzle periods");
+  const char* const kp = static_cast<const char*>(a.k_pages) + 2 * (long long)u.g * a.c.head_stride;
+  const char* const vp = static_cast<const char*>(a.v_pages) + 2 * (long long)u.g * a.c.head_stride;
+  auto issue = [&](int ti, int page, auto& Kb, auto& Vb) -> unsigned long long {
+    const int t = ti * PA_TILE + lane, tc = min(t, len - 1);
+    const bool there = page >= 0 && page < a.c.n_pages;
+    if (!there && t < len) atomicOr(a.fault, DSBD_FAULT_BOUNDS);
+    const long long off = there ? 2 * ((long long)page * a.c.page_stride + (long long)(tc - quotient(a.c.page, tc) * a.c.page.d) * a.c.token_stride) : -1;
+#pragma unroll
+    for (int r = 0; r < ROUNDS; ++r) {
+      const int from = 4 * TPI * r + ld_tok;
+      const int lo = __shfl((int)(unsigned)off, from), hi = __shfl((int)(off >> 32), from);
+      const long long o = ((long long)hi << 32) | (unsigned)lo;
+      const char* const ks = o >= 0 ? kp + o + 16 * ld_k : static_cast<const char*>(a.q);
+      const char* const vs = o >= 0 ? vp + o + 16 * ld_v : static_cast<const char*>(a.q);
+      __builtin_amdgcn_global_load_lds((glb_cvoid*)ks, (lds_void*)&Kb[(4 * r + wave) * 64], 16, 0, 0);
+      __builtin_amdgcn_global_load_lds((glb_cvoid*)vs, (lds_void*)&Vb[(4 * r + wave) * 64], 16, 0, 0);
+    }
+    return __ballot(there && t < len);
+  };
+
+  // ---- query rows
+  x8 qf[RT][DS];
+  int limit[RT];
+  uint64_t anc[RT];
+#pragma unroll
+  for (int rt = 0; rt < RT; ++rt) {
+    const int r = row0 + wave * ROWS_W + 32 * rt + col;
+    const bool live = r < R;
+    const int tok = quotient(a.group, live ? r : row0), head = u.g * a.group.d + (live ? r - tok * a.group.d : 0);
+    limit[rt] = live ? sq.ctx + tok + 1 : 0;
+    anc[rt] = live && a.anc ? a.anc[sq.first + tok] : 0ull;
+    const T* qp = static_cast<const T*>(a.q) + (long long)(sq.first + tok) * a.q_tok + head * a.q_head + 8 * h;
+#pragma unroll
+    for (int j = 0; j < DS; ++j) {
+      union { u32x4 u; x8 v; } c;
+      c.u = u32x4{0, 0, 0, 0};
+      if (live) c.u = *(const gvec*)(qp + 16 * j);
+      qf[rt][j] = c.v;
+    }
+  }
+  floatx16 o[RT][DT];
+  float m_ref[RT], l_run[RT];
+#pragma unroll
+  for (int rt = 0; rt < RT; ++rt) {
+    m_ref[rt] = -INFINITY; l_run[rt] = 0.f;
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) o[rt][dt][i] = 0.f;
+  }
+  // byte offsets of the operand reads inside a tile: K token col, piece 2j + h; V token 4h + (lane % 16) / 4, channels
+  // 16 * (lane / 16 % 2) + 4 * (lane % 4) of a tile of 32
+  int k_off[DS], v_off[DT];
+#pragma unroll
+  for (int j = 0; j < DS; ++j) k_off[j] = col * ROWB + (((2 * j + h) ^ swz_k(col)) << 4);
+  {
+    const int t = 4 * h + ((lane & 15) >> 2), c = 16 * ((lane >> 4) & 1) + 4 * (lane & 3);
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt) v_off[dt] = t * ROWB + (((4 * dt + (c >> 3)) ^ swz_v(t)) << 4) + ((c & 4) << 1);
+  }
+
+  auto scores = [&](int hf, const char* kl, floatx16 (&s)[RT]) __attribute__((always_inline)) {
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) s[rt][i] = 0.f;
+#pragma unroll
+    for (int j = 0; j < DS; ++j) {
+      const x8 kf = *reinterpret_cast<const x8*>(kl + 32 * hf * ROWB + k_off[j]);
+#pragma unroll
+      for (int rt = 0; rt < RT; ++rt) s[rt] = Elem<T>::mfma(kf, qf[rt][j], s[rt]);
+    }
+  };
+  auto soften = [&](bool masked, uint32_t valid, int tok0, floatx16 (&s)[RT], x8 (&pf)[RT][2]) __attribute__((always_inline)) {
+    if (masked) {
+#pragma unroll
+      for (int rt = 0; rt < RT; ++rt) {
+        const uint32_t b = (valid & (limit[rt] ? seen_bits(a, tok0, limit[rt], sq.ctx, anc[rt]) : 0u)) >> (4 * h);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) if (!((b >> (8 * (i >> 2) + (i & 3))) & 1)) s[rt][i] = -INFINITY;
+      }
+    }
+    bool raise = false;
+    float mx[RT];
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+      mx[rt] = s[rt][0];
+#pragma unroll
+      for (int i = 1; i < 16; ++i) mx[rt] = fmaxf(mx[rt], s[rt][i]);
+      mx[rt] *= a.scale_log2;
+      raise |= mx[rt] > m_ref[rt] + Elem<T>::SLACK;
+    }
+    if (__any(raise)) {
+#pragma unroll
+      for (int rt = 0; rt < RT; ++rt) {
+        const float m = fmaxf(mx[rt], __shfl_xor(mx[rt], 32));
+        if (m > m_ref[rt] + Elem<T>::SLACK) {
+          const float to = m - Elem<T>::SHIFT;
+          const float f = m_ref[rt] == -INFINITY ? 0.f : exp2f(m_ref[rt] - to);
+          m_ref[rt] = to;
+          l_run[rt] *= f;
+#pragma unroll
+          for (int dt = 0; dt < DT; ++dt) o[rt][dt] *= f;
+        }
+      }
+    }
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+      const float ref = m_ref[rt] == -INFINITY ? 0.f : -m_ref[rt];
+      float sum = 0.f;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const float p = __builtin_amdgcn_exp2f(fmaf(s[rt][i], a.scale_log2, ref));
+        sum += p;
+        pf[rt][i >> 3][i & 7] = (T)p;
+      }
+      l_run[rt] += sum;
+    }
+  };
+  auto weigh = [&](int hf, const char* vl, const x8 (&pf)[RT][2]) __attribute__((always_inline)) {
+#pragma unroll
+    for (int ks = 0; ks < 2; ++ks)
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt) {
+        union { v4i16 q[2]; x8 v; } vf;
+        const char* const rowp = vl + (32 * hf + 16 * ks) * ROWB + v_off[dt];
+        vf.q[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4i16*)(rowp));
+        vf.q[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4i16*)(rowp + 8 * ROWB));
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt) o[rt][dt] = Elem<T>::mfma(vf.v, pf[rt][ks], o[rt][dt]);
+      }
+  };
+  auto compute = [&](int ti, unsigned long long valid, auto& Kb, auto& Vb) __attribute__((always_inline)) {
+    const char* const kl = reinterpret_cast<const char*>(&Kb[0]);
+    const char* const vl = reinterpret_cast<const char*>(&Vb[0]);
+    const int tok0 = ti * PA_TILE;
+    const bool masked = valid != ~0ull || tok0 + PA_TILE > open;
+    if (masked) {
+      // NaN or Inf among values that not all rows see: a product with a numerator of 0 would be NaN, so they leave the tile,
+      // and the rows that see them are marked.
+      for (int i = threadIdx.x; i < PA_TILE * PPR; i += PA_BLOCK) {
+        if (!any_nonfinite<T>(Vb[i])) continue;
+        const int t = i / PPR, piece = (i % PPR) ^ swz_v(t);
+        unsigned short* const e = reinterpret_cast<unsigned short*>(&Vb[i]);
+        for (int k = 0; k < 8; ++k) {
+          const unsigned short x = e[k];
+          if ((x & Elem<T>::INF) != Elem<T>::INF) continue;
+          e[k] = 0;
+          if (!((valid >> t) & 1)) continue;
+          const int c = 8 * piece + k;
+          const unsigned kind = (x & 0x7fffu) != Elem<T>::INF ? 3u : x & 0x8000u ? 2u : 1u;
+          for (int rl = 0; rl < ROWS && row0 + rl < R; ++rl) {
+            const int tok = quotient(a.group, row0 + rl);
+            const bool sees = a.anc ? tok0 + t < sq.ctx || ((a.anc[sq.first + tok] >> (tok0 + t - sq.ctx)) & 1) : tok0 + t <= sq.ctx + tok;
+            if (sees) atomicOr(&lost[rl][c / 16], kind << (2 * (c % 16)));
+          }
+          any_lost = 1;
+        }
+      }
+      lds_barrier();
+    }
+#pragma unroll
+    for (int hf = 0; hf < 2; ++hf) {
+      floatx16 s[RT];
+      x8 pf[RT][2];
+      scores(hf, kl, s);
+      soften(masked, (uint32_t)(valid >> (32 * hf)), tok0 + 32 * hf, s, pf);
+      weigh(hf, vl, pf);
+    }
+  };
+
+  for (int i = threadIdx.x; i < ROWS * (D / 16); i += PA_BLOCK) lost[i / (D / 16)][i % (D / 16)] = 0;
+  if (threadIdx.x == 0) any_lost = 0;
+  int ti = t_begin, page = 0;
+  unsigned long long valid_a = 0, valid_b = 0;
+  if (ti < t_end) {
+    page = look_up(ti);
+    valid_a = issue(ti, page, kA, vA);
+    if (ti + 1 < t_end) page = look_up(ti + 1);
+  }
+  // One barrier per tile: every wave's part of it has landed, and everybody is done with the buffer that is filled next.
+  while (ti < t_end) {
+    __builtin_amdgcn_s_waitcnt(0x0F70);        // vmcnt(0)
+    lds_barrier();
+    if (ti + 1 < t_end) { valid_b = issue(ti + 1, page, kB, vB); if (ti + 2 < t_end) page = look_up(ti + 2); }
+    compute(ti, valid_a, kA, vA);
+    if (++ti >= t_end) break;
+    __builtin_amdgcn_s_waitcnt(0x0F70);
+    lds_barrier();
+    if (ti + 1 < t_end) { valid_a = issue(ti + 1, page, kA, vA); if (ti + 2 < t_end) page = look_up(ti + 2); }
+    compute(ti, valid_b, kB, vB);
+    ++ti;
+  }
+  __syncthreads();                             // the buffers become the output staging: an array per wave
+#pragma unroll
+  for (int rt = 0; rt < RT; ++rt) l_run[rt] += __shfl_xor(l_run[rt], 32);
+  uint4* const stage = wave == 0 ? kA : wave == 1 ? kB : wave == 2 ? vA : vB;
+  constexpr int QPR = D / 4, HALF = QPR / 2;   // 4-channel pieces of a row; they go through the LDS half a row at a time
+#pragma unroll
+  for (int rt = 0; rt < RT; ++rt) {
+    const int rw = wave * ROWS_W + 32 * rt;
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+      wave_lds_fence();
+#pragma unroll
+      for (int dt = 0; dt < DT / 2; ++dt)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          union { floatx4 f; uint4 u; } c;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) c.f[i] = o[rt][half * (DT / 2) + dt][4 * k + i];
+          stage[col * HALF + ((8 * dt + 2 * k + h) ^ (col & 7))] = c.u;
+        }
+      wave_lds_fence();
+#pragma unroll 4
+      for (int i = lane; i < 32 * HALF; i += 64) {
+        const int rl = i / HALF, q = i % HALF, part = half * HALF + q, r = row0 + rw + rl;
+        const float M = __shfl(m_ref[rt], rl), L = __shfl(l_run[rt], rl);
+        if (r >= R) continue;
+        union { uint4 u; floatx4 f; } c;
+        c.u = stage[rl * HALF + (q ^ (rl & 7))];
+        const int tok = quotient(a.group, r), head = u.g * a.group.d + r - tok * a.group.d;
+        const long long row = sq.first + tok, slot = (long long)blockIdx.x * ROWS + rw + rl;
+        const unsigned gone = any_lost ? (lost[rw + rl][part / 4] >> (8 * (part % 4))) & 255u : 0u;
+        if (u.nparts == 1) {
+          write_row<T, D>(a, row, head, part, M, L, c.f, gone);
+        } else {
+          if (gone) {
+            unsigned* const b = reinterpret_cast<unsigned*>(&c.u);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) if (const unsigned x = (gone >> (2 * k)) & 3) b[k] = x == 1 ? 0x7f800000u : x == 2 ? 0xff800000u : 0x7fc00000u;
+          }
+          *reinterpret_cast<uint4*>(&a.part_o[slot * D + 4 * part]) = c.u;
+          if (part == 0) { a.part_ml[2 * slot] = M; a.part_ml[2 * slot + 1] = L; }
+        }
+        if (a.splits && part == 0 && u.part == 0) a.row_parts[row * a.Hq + head] = make_int2((int)slot, u.nparts);
+      }
+    }
+  }
+}
+
 // A wave per (row, head) of what was split: the parts of a unit are Hkv * rows apart.
 template <typename T, int D>
 __global__ __launch_bounds__(PA_BLOCK) void paged_join_kernel(PagedAttnArgs a) {
@@ -451,18 +751,19 @@ __global__ __launch_bounds__(PA_BLOCK) void paged_join_kernel(PagedAttnArgs a) {
 
 // How a call is cut up.
 struct Plan {
-  int rows;                  // per block
+  int rows;                  // per block: 16 and 32 wave-private, 128 tiles
   long long grid;
   bool splits;
   size_t bytes;
 };
 Plan plan(const dsbd_paged_kv* c, int n_rows, int Hq, int Hkv, int D, PagedAttnArgs* a, void* workspace) {
   Plan p;
-  const long long group = Hq / Hkv;
-  p.rows = (long long)c->max_new * group <= 16 ? 16 : 32;
+  const long long group = Hq / Hkv, most = (long long)std::min(c->max_new, n_rows) * group;     // rows of a sequence and KV head
+  p.rows = most <= 16 ? 16 : most <= 32 ? 32 : 128;
+  const long long slots = p.rows <= 32 ? PA_SLOTS : PA_TILE_SLOTS;
   const long long units = ((long long)n_rows * group / p.rows + c->n_seqs) * Hkv;      // at most
-  p.splits = units < 2 * PA_SLOTS;
-  p.grid = units + (p.splits ? PA_SLOTS : 0);
+  p.splits = units < 2 * slots;
+  p.grid = units + (p.splits ? slots : 0);
   WorkspaceCarver w(workspace);
   float *po = nullptr, *ml = nullptr;
   int2* rp = nullptr;
@@ -526,7 +827,8 @@ extern "C" int32_t dsbd_paged_attention(const dsbd_paged_kv* cache, int32_t n_ro
 #define PA_ROWS(T, DD)                                                                                     \
   do {                                                                                                     \
     if (p.rows == 16) hipLaunchKernelGGL((paged_wave_kernel<T, DD, 1>), grid, block, 0, stream, a);        \
-    else hipLaunchKernelGGL((paged_wave_kernel<T, DD, 2>), grid, block, 0, stream, a);                     \
+    else if (p.rows == 32) hipLaunchKernelGGL((paged_wave_kernel<T, DD, 2>), grid, block, 0, stream, a);   \
+    else hipLaunchKernelGGL((paged_tile_kernel<T, DD, 1>), grid, block, 0, stream, a);                     \
     DSBD_HIP_LAUNCH_CHECK();                                                                               \
     if (p.splits) hipLaunchKernelGGL((paged_join_kernel<T, DD>), join, block, 0, stream, a);               \
   } while (0)
