@@ -58,7 +58,7 @@ struct PagedAttnArgs {
   int n_rows, Hq, Hkv;
   FastDiv group, heads;                        // query heads per KV head; KV heads
   float scale_log2;                            // scale * log2(e): scores are kept in the log2 domain
-  int page_run;                                // pages are whole multiples of this many tokens (8, or 1)
+  int page_run;                                // pages are whole multiples of this many tokens (1, 8, 16 or 32)
   int splits;                                  // whether units may be split
   float* part_o;                               // [grid][rows per block][D]
   float* part_ml;                              // [grid][rows per block][2]
@@ -459,36 +459,54 @@ __global__ __launch_bounds__(PA_BLOCK, RT == 1 ? 2 : 1) void paged_tile_kernel(P
   const int upto = !sq.good ? 0 : a.anc ? len : sq.ctx + last_tok + 1;
   const int tiles = (upto + PA_TILE - 1) / PA_TILE;
   const int t_begin = u.nparts == 1 ? 0 : (int)min((long long)u.part * part_tiles, (long long)tiles);
-  const int t_end = u.nparts == 1 ? tiles : min(tiles, t_begin + part_tiles);
+  const int t_end = a.c.n_pages == 0 ? t_begin : u.nparts == 1 ? tiles : min(tiles, t_begin + part_tiles);
+  if (a.c.n_pages == 0 && threadIdx.x == 0) atomicOr(a.fault, DSBD_FAULT_BOUNDS);
   const int open = sq.ctx + (a.anc ? 0 : first_tok + 1);      // tokens in front of this are seen by all rows
 
-  // ---- where tokens lie: lane l looks up token l of a tile; invalid ones read the first query row instead, and are masked
+  // ---- where tokens lie: lane l looks up token l of a tile.  Tokens without a page read page 0, tokens behind the last whatever is
+  // in the last one's page; both are masked.
   const int32_t* const table = a.c.page_table + (long long)u.s * a.c.table_stride;
-  auto look_up = [&](int ti) { const int t = min(ti * PA_TILE + lane, len - 1), p = quotient(a.c.page, t);
-    return p < a.c.table_stride ? table[p] : -1; };
+  auto look_up = [&](int ti) {
+    const int p = quotient(a.c.page, min(ti * PA_TILE + lane, len - 1));
+    return p < a.c.table_stride ? table[p] : -1;
+  };
   // swizzles: K is read down 16 tokens at one piece, V down 8 tokens at 4 pieces in a row
   auto swz_k = [](int t) { return D == 128 ? t & 15 : (t >> 1) & 7; };
   auto swz_v = [](int t) { return D == 128 ? 4 * (t & 3) : 4 * ((t >> 1) & 1); };
+  constexpr int RUN = 4 * TPI;                 // tokens per round of the four waves
   const int ld_tok = TPI * wave + lane / PPR, ld_k = (lane % PPR) ^ swz_k(ld_tok), ld_v = (lane % PPR) ^ swz_v(ld_tok);
-  static_assert((4 * TPI) % 16 == 0, "a round is a whole number of swizzle periods");
+  static_assert(RUN % 16 == 0, "a round is a whole number of swizzle periods");
   const char* const kp = static_cast<const char*>(a.k_pages) + 2 * (long long)u.g * a.c.head_stride;
   const char* const vp = static_cast<const char*>(a.v_pages) + 2 * (long long)u.g * a.c.head_stride;
-  auto issue = [&](int ti, int page, auto& Kb, auto& Vb) -> unsigned long long {
-    const int t = ti * PA_TILE + lane, tc = min(t, len - 1);
+  const unsigned k_lane = (unsigned)(ld_tok * 2 * (int)a.c.token_stride + 16 * ld_k), v_lane = (unsigned)(ld_tok * 2 * (int)a.c.token_stride + 16 * ld_v);
+  auto issue = [&](int ti, int page, auto& Kb, auto& Vb) __attribute__((always_inline)) -> unsigned long long {
+    const int t = ti * PA_TILE + lane;
     const bool there = page >= 0 && page < a.c.n_pages;
-    if (!there && t < len) atomicOr(a.fault, DSBD_FAULT_BOUNDS);
-    const long long off = there ? 2 * ((long long)page * a.c.page_stride + (long long)(tc - quotient(a.c.page, tc) * a.c.page.d) * a.c.token_stride) : -1;
+    const unsigned long long valid = __ballot(there && t < len);
+    if (valid != ~0ull && !there && t < len) atomicOr(a.fault, DSBD_FAULT_BOUNDS);
+    page = there ? page : 0;
+    if (a.page_run >= RUN) {
+      // a round's tokens lie in one page: its place is worked out once, for the wave
 #pragma unroll
-    for (int r = 0; r < ROUNDS; ++r) {
-      const int from = 4 * TPI * r + ld_tok;
-      const int lo = __shfl((int)(unsigned)off, from), hi = __shfl((int)(off >> 32), from);
-      const long long o = ((long long)hi << 32) | (unsigned)lo;
-      const char* const ks = o >= 0 ? kp + o + 16 * ld_k : static_cast<const char*>(a.q);
-      const char* const vs = o >= 0 ? vp + o + 16 * ld_v : static_cast<const char*>(a.q);
-      __builtin_amdgcn_global_load_lds((glb_cvoid*)ks, (lds_void*)&Kb[(4 * r + wave) * 64], 16, 0, 0);
-      __builtin_amdgcn_global_load_lds((glb_cvoid*)vs, (lds_void*)&Vb[(4 * r + wave) * 64], 16, 0, 0);
+      for (int r = 0; r < ROUNDS; ++r) {
+        const int tok = min(ti * PA_TILE + RUN * r, (len - 1) & ~(RUN - 1));
+        const long long off = 2 * ((long long)__builtin_amdgcn_readlane(page, RUN * r) * a.c.page_stride +
+                                   (long long)(tok - quotient(a.c.page, tok) * a.c.page.d) * a.c.token_stride);
+        __builtin_amdgcn_global_load_lds((glb_cvoid*)(kp + off + k_lane), (lds_void*)&Kb[(4 * r + wave) * 64], 16, 0, 0);
+        __builtin_amdgcn_global_load_lds((glb_cvoid*)(vp + off + v_lane), (lds_void*)&Vb[(4 * r + wave) * 64], 16, 0, 0);
+      }
+    } else {
+      const int tc = min(t, len - 1);
+      const long long off = 2 * ((long long)page * a.c.page_stride + (long long)(tc - quotient(a.c.page, tc) * a.c.page.d) * a.c.token_stride);
+#pragma unroll
+      for (int r = 0; r < ROUNDS; ++r) {
+        const int lo = __shfl((int)(unsigned)off, RUN * r + ld_tok), hi = __shfl((int)(off >> 32), RUN * r + ld_tok);
+        const long long o = ((long long)hi << 32) | (unsigned)lo;
+        __builtin_amdgcn_global_load_lds((glb_cvoid*)(kp + o + 16 * ld_k), (lds_void*)&Kb[(4 * r + wave) * 64], 16, 0, 0);
+        __builtin_amdgcn_global_load_lds((glb_cvoid*)(vp + o + 16 * ld_v), (lds_void*)&Vb[(4 * r + wave) * 64], 16, 0, 0);
+      }
     }
-    return __ballot(there && t < len);
+    return valid;
   };
 
   // ---- query rows
@@ -544,22 +562,23 @@ __global__ __launch_bounds__(PA_BLOCK, RT == 1 ? 2 : 1) void paged_tile_kernel(P
       for (int rt = 0; rt < RT; ++rt) s[rt] = Elem<T>::mfma(kf, qf[rt][j], s[rt]);
     }
   };
-  auto soften = [&](bool masked, uint32_t valid, int tok0, floatx16 (&s)[RT], x8 (&pf)[RT][2]) __attribute__((always_inline)) {
-    if (masked) {
+  auto mask = [&](uint32_t valid, int tok0, floatx16 (&s)[RT]) __attribute__((always_inline)) {
 #pragma unroll
-      for (int rt = 0; rt < RT; ++rt) {
-        const uint32_t b = (valid & (limit[rt] ? seen_bits(a, tok0, limit[rt], sq.ctx, anc[rt]) : 0u)) >> (4 * h);
+    for (int rt = 0; rt < RT; ++rt) {
+      const uint32_t b = (valid & (limit[rt] ? seen_bits(a, tok0, limit[rt], sq.ctx, anc[rt]) : 0u)) >> (4 * h);
 #pragma unroll
-        for (int i = 0; i < 16; ++i) if (!((b >> (8 * (i >> 2) + (i & 3))) & 1)) s[rt][i] = -INFINITY;
-      }
+      for (int i = 0; i < 16; ++i) if (!((b >> (8 * (i >> 2) + (i & 3))) & 1)) s[rt][i] = -INFINITY;
     }
+  };
+  // the rows' references, raised where a score of the tile is too far above
+  auto refer = [&](const floatx16 (&s0)[RT], const floatx16 (&s1)[RT]) __attribute__((always_inline)) {
     bool raise = false;
     float mx[RT];
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
-      mx[rt] = s[rt][0];
+      mx[rt] = fmaxf(s0[rt][0], s1[rt][0]);
 #pragma unroll
-      for (int i = 1; i < 16; ++i) mx[rt] = fmaxf(mx[rt], s[rt][i]);
+      for (int i = 1; i < 16; ++i) mx[rt] = fmaxf(mx[rt], fmaxf(s0[rt][i], s1[rt][i]));
       mx[rt] *= a.scale_log2;
       raise |= mx[rt] > m_ref[rt] + Elem<T>::SLACK;
     }
@@ -577,6 +596,8 @@ __global__ __launch_bounds__(PA_BLOCK, RT == 1 ? 2 : 1) void paged_tile_kernel(P
         }
       }
     }
+  };
+  auto soften = [&](const floatx16 (&s)[RT], x8 (&pf)[RT][2]) __attribute__((always_inline)) {
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
       const float ref = m_ref[rt] == -INFINITY ? 0.f : -m_ref[rt];
@@ -632,14 +653,16 @@ __global__ __launch_bounds__(PA_BLOCK, RT == 1 ? 2 : 1) void paged_tile_kernel(P
       }
       lds_barrier();
     }
-#pragma unroll
-    for (int hf = 0; hf < 2; ++hf) {
-      floatx16 s[RT];
-      x8 pf[RT][2];
-      scores(hf, kl, s);
-      soften(masked, (uint32_t)(valid >> (32 * hf)), tok0 + 32 * hf, s, pf);
-      weigh(hf, vl, pf);
-    }
+    floatx16 s0[RT], s1[RT];
+    x8 p0[RT][2], p1[RT][2];
+    scores(0, kl, s0);
+    scores(1, kl, s1);
+    if (masked) { mask((uint32_t)valid, tok0, s0); mask((uint32_t)(valid >> 32), tok0 + 32, s1); }
+    refer(s0, s1);
+    soften(s0, p0);
+    weigh(0, vl, p0);
+    soften(s1, p1);
+    weigh(1, vl, p1);
   };
 
   for (int i = threadIdx.x; i < ROWS * (D / 16); i += PA_BLOCK) lost[i / (D / 16)][i % (D / 16)] = 0;
@@ -819,7 +842,9 @@ extern "C" int32_t dsbd_paged_attention(const dsbd_paged_kv* cache, int32_t n_ro
   a.q_tok = q->token_stride; a.q_head = q->head_stride; a.o_tok = out->token_stride; a.o_head = out->head_stride;
   a.n_rows = n_rows; a.Hq = Hq; a.Hkv = Hkv; a.group = fast_div(Hq / Hkv); a.heads = fast_div(Hkv);
   a.scale_log2 = (float)((scale > 0.f ? (double)scale : 1.0 / sqrt((double)D)) * 1.4426950408889634);
-  a.page_run = cache->page_size % 8 == 0 ? 8 : 1;
+  // (the tile kernel's short way adds a lane's place in a run of tokens as a 32-bit number of bytes)
+  a.page_run = cache->page_size % 32 == 0 ? 32 : cache->page_size % 16 == 0 ? 16 : cache->page_size % 8 == 0 ? 8 : 1;
+  if (cache->token_stride >= (1 << 25)) a.page_run = std::min(a.page_run, 8);
   a.fault = fault;
   hipStream_t stream = static_cast<hipStream_t>(stream_);
   const dim3 grid((unsigned)p.grid), block(PA_BLOCK);
