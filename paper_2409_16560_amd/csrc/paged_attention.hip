@@ -19,7 +19,8 @@ namespace {
 #define PA_STEP 32                 // tokens per wave step
 #define PA_SLOTS 512               // workgroups of the wave-private kernel that the device holds (70 KB of LDS each)
 #define PA_MIN_STEPS 4             // steps that a part has at least
-#define PA_TILE_SLOTS 512           // workgroups of the tile kernel that the device holds
+#define PA_TILE_BLOCK 512
+#define PA_TILE_SLOTS 256           // workgroups of the tile kernel that the device holds
 
 typedef float floatx4 __attribute__((ext_vector_type(4)));
 typedef float floatx16 __attribute__((ext_vector_type(16)));
@@ -35,14 +36,14 @@ typedef __attribute__((address_space(1))) u32x4 gvec;
 template <typename T> struct Elem;
 template <> struct Elem<__bf16> {
   typedef __bf16 x8 __attribute__((ext_vector_type(8)));
-  static constexpr float SLACK = 40.f, SHIFT = 0.f;
+  static constexpr float SLACK = 40.f, SHIFT = 0.f, MOST = 0x1p60f;
   static __device__ __forceinline__ floatx4 mfma(x8 a, x8 b, floatx4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
   static __device__ __forceinline__ floatx16 mfma(x8 a, x8 b, floatx16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
   static constexpr unsigned INF = 0x7f80u;
 };
 template <> struct Elem<_Float16> {
   typedef _Float16 x8 __attribute__((ext_vector_type(8)));
-  static constexpr float SLACK = 15.f, SHIFT = 8.f;
+  static constexpr float SLACK = 15.f, SHIFT = 8.f, MOST = 0x1p15f;
   static __device__ __forceinline__ floatx4 mfma(x8 a, x8 b, floatx4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
   static __device__ __forceinline__ floatx16 mfma(x8 a, x8 b, floatx16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
   static constexpr unsigned INF = 0x7c00u;
@@ -58,13 +59,14 @@ struct PagedAttnArgs {
   int n_rows, Hq, Hkv;
   FastDiv group, heads;                        // query heads per KV head; KV heads
   float scale_log2;                            // scale * log2(e): scores are kept in the log2 domain
-  int page_run;                                // pages are whole multiples of this many tokens (1, 8, 16 or 32)
+  int page_run;                                // pages are whole multiples of this many tokens (8, or 1)
   int splits;                                  // whether units may be split
   float* part_o;                               // [grid][rows per block][D]
   float* part_ml;                              // [grid][rows per block][2]
   int2* row_parts;                             // [n_rows*Hq] first partial row, how many parts
   long long part_rows;                         // rows of part_o
   int block_rows;
+  int per_die;                                 // Hkv a multiple of 8: workgroups per KV head
   int32_t* fault;
 };
 
@@ -88,8 +90,17 @@ struct Unit { int s, g, rb, part, nparts; };
 template <int STEP>
 __device__ __forceinline__ bool find_unit(const PagedAttnArgs& a, int slots, Unit& u, int& part_steps) {
   const int lane = threadIdx.x & 63, rows = a.block_rows;
-  const int at = quotient(a.heads, blockIdx.x);
-  u.g = blockIdx.x - at * a.Hkv;
+  // Workgroups go to the 8 dies in turn: with 8 heads or a multiple a die takes its heads one after the other, so that what it has in
+  // hand shares the keys in its L2.
+  int at;
+  if (a.per_die) {
+    const int idx = blockIdx.x >> 3, k = idx / a.per_die;
+    u.g = (blockIdx.x & 7) + 8 * k;
+    at = idx - k * a.per_die;
+  } else {
+    at = quotient(a.heads, blockIdx.x);
+    u.g = blockIdx.x - at * a.Hkv;
+  }
   auto measure = [&](int s, int& nrb, int& steps) {
     nrb = 0; steps = 0;
     if (s < a.c.n_seqs) {
@@ -425,26 +436,38 @@ __global__ __launch_bounds__(PA_BLOCK) void paged_wave_kernel(PagedAttnArgs a) {
 
 // ---- tile kernel: many rows on the same keys
 //
-// Four waves of 32 * RT rows each share tiles of 64 tokens of K and V in the LDS, two of each, filled by direct loads (no
-// registers in between) a tile ahead; the pieces of a row are swizzled by the token, so that the operand reads, which go down the
-// rows, spread over the banks.  MFMA 32x32x16: S^T = K Q^T and O^T += V^T P^T as in the wave-private kernel, a lane owns a query
-// row together with the lane 32 further on, which has the other half of its tokens.
+// Eight waves of 32 rows share tiles of 64 tokens of K and V in the LDS, a ring of three of each, filled by direct loads (no registers
+// in between); the pieces of a row are swizzled by the token, so that the operand reads, which go down the rows, spread over the
+// banks.  MFMA 32x32x16: S^T = K Q^T and O^T += V^T P^T as in the wave-private kernel; a lane owns a query row together with the
+// lane 32 further on, which has the other half of its tokens.
+// Two phases take turns: 32 matrix instructions (V of the tile before, K of this one) and the exponentials of a tile.  The waves
+// of a SIMD, w and w + 4, are always in different ones, with a barrier between phases: left to themselves they run in step,
+// both waiting for the matrix unit and then both for the vector unit.
 #define PA_TILE 64
 
-typedef __attribute__((address_space(3))) void lds_void;
-typedef const __attribute__((address_space(1))) void glb_cvoid;
+typedef __attribute__((address_space(3))) char lds_char;
 
 // Workgroup barrier that orders LDS traffic only (loads in flight stay in flight).
 __device__ __forceinline__ void lds_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+// 16 bytes per lane from base + its offset to consecutive places in the LDS.  (Written out: behind the compiler's own form of
+// it every LDS read waits for all such loads, whatever part of the LDS they fill.  No register is written.)
+__device__ __forceinline__ void load_to_lds(unsigned lds, const char* base, unsigned lane_offset) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(lane_offset), "s"(base) : "memory");
+}
+__device__ __forceinline__ void load_to_lds(unsigned lds, const char* from) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds), "v"(from) : "memory");
+}
 
-template <typename T, int D, int RT>
-__global__ __launch_bounds__(PA_BLOCK, RT == 1 ? 2 : 1) void paged_tile_kernel(PagedAttnArgs a) {
+// RUNS: pages are whole multiples of 8 tokens.
+template <typename T, int D, bool RUNS>
+__global__ __launch_bounds__(PA_TILE_BLOCK, 2) void paged_tile_kernel(PagedAttnArgs a) {
   typedef typename Elem<T>::x8 x8;
+  constexpr int NW = PA_TILE_BLOCK / 64, ROWS = 32 * NW;
   constexpr int DS = D / 16, DT = D / 32;               // k-steps of S^T, channel tiles of O^T
-  constexpr int ROWS_W = 32 * RT, ROWS = 4 * ROWS_W;
   constexpr int PPR = D / 8, ROWB = 2 * D;              // 16-byte pieces and bytes of a row
-  constexpr int TPI = 64 / PPR, ROUNDS = PA_TILE / (4 * TPI);     // tokens per load instruction, instructions per wave and tile
-  __shared__ uint4 kA[PA_TILE * PPR], kB[PA_TILE * PPR], vA[PA_TILE * PPR], vB[PA_TILE * PPR];
+  constexpr int TPI = 64 / PPR, RUN = NW * TPI, ROUNDS = PA_TILE / RUN;      // tokens per load instruction, and of all waves; instructions per tile
+  constexpr int TILE_BYTES = PA_TILE * ROWB;
+  __shared__ __attribute__((aligned(16))) char ring[6 * TILE_BYTES];         // three tiles of K, three of V
   // two bits per row and channel whose sum is +Inf, -Inf or NaN (both)
   __shared__ unsigned lost[ROWS][D / 16];
   __shared__ int any_lost;
@@ -463,274 +486,302 @@ __global__ __launch_bounds__(PA_BLOCK, RT == 1 ? 2 : 1) void paged_tile_kernel(P
   if (a.c.n_pages == 0 && threadIdx.x == 0) atomicOr(a.fault, DSBD_FAULT_BOUNDS);
   const int open = sq.ctx + (a.anc ? 0 : first_tok + 1);      // tokens in front of this are seen by all rows
 
-  // ---- where tokens lie: lane l looks up token l of a tile.  Tokens without a page read page 0, tokens behind the last whatever is
-  // in the last one's page; both are masked.
+  // ---- where tokens lie.  Tokens without a page read page 0, tokens behind the last whatever is in the last one's page; both are
+  // masked.
   const int32_t* const table = a.c.page_table + (long long)u.s * a.c.table_stride;
-  auto look_up = [&](int ti) {
-    const int p = quotient(a.c.page, min(ti * PA_TILE + lane, len - 1));
-    return p < a.c.table_stride ? table[p] : -1;
-  };
   // swizzles: K is read down 16 tokens at one piece, V down 8 tokens at 4 pieces in a row
   auto swz_k = [](int t) { return D == 128 ? t & 15 : (t >> 1) & 7; };
   auto swz_v = [](int t) { return D == 128 ? 4 * (t & 3) : 4 * ((t >> 1) & 1); };
-  constexpr int RUN = 4 * TPI;                 // tokens per round of the four waves
   const int ld_tok = TPI * wave + lane / PPR, ld_k = (lane % PPR) ^ swz_k(ld_tok), ld_v = (lane % PPR) ^ swz_v(ld_tok);
   static_assert(RUN % 16 == 0, "a round is a whole number of swizzle periods");
   const char* const kp = static_cast<const char*>(a.k_pages) + 2 * (long long)u.g * a.c.head_stride;
   const char* const vp = static_cast<const char*>(a.v_pages) + 2 * (long long)u.g * a.c.head_stride;
-  const unsigned k_lane = (unsigned)(ld_tok * 2 * (int)a.c.token_stride + 16 * ld_k), v_lane = (unsigned)(ld_tok * 2 * (int)a.c.token_stride + 16 * ld_v);
-  auto issue = [&](int ti, int page, auto& Kb, auto& Vb) __attribute__((always_inline)) -> unsigned long long {
-    const int t = ti * PA_TILE + lane;
-    const bool there = page >= 0 && page < a.c.n_pages;
-    const unsigned long long valid = __ballot(there && t < len);
-    if (valid != ~0ull && !there && t < len) atomicOr(a.fault, DSBD_FAULT_BOUNDS);
-    page = there ? page : 0;
-    if (a.page_run >= RUN) {
-      // a round's tokens lie in one page: its place is worked out once, for the wave
+  const unsigned k_lane = (unsigned)(lane / PPR * 2 * (int)a.c.token_stride + 16 * ld_k), v_lane = (unsigned)(lane / PPR * 2 * (int)a.c.token_stride + 16 * ld_v);
+  const unsigned ring_at = (unsigned)(uintptr_t)(lds_char*)ring;
+  // lane l: the page of token l of a tile
+  auto look_up = [&](int ti) __attribute__((always_inline)) {
+    const int p = quotient(a.c.page, min(ti * PA_TILE + lane, len - 1));
+    return p < a.c.table_stride ? table[p] : -1;
+  };
+  // which tokens of a tile are there, a bit each
+  auto present = [&](int ti, int page) __attribute__((always_inline)) {
+    const int n = len - ti * PA_TILE;
+    const unsigned long long inside = n >= 64 ? ~0ull : (1ull << n) - 1, valid = __ballot(page >= 0 && page < a.c.n_pages);
+    if (inside & ~valid) atomicOr(a.fault, DSBD_FAULT_BOUNDS);
+    return valid & inside;
+  };
+  // where token l of a tile lies, in bytes (RUNS: where the run of tokens that a load instruction takes begins, which lies in one page)
+  auto offset = [&](int ti, int page) __attribute__((always_inline)) {
+    const int t = min(ti * PA_TILE + lane, RUNS ? (len - 1) & ~(TPI - 1) : len - 1);
+    page = page >= 0 && page < a.c.n_pages ? page : 0;
+    return 2 * ((long long)page * a.c.page_stride + (long long)(t - quotient(a.c.page, t) * a.c.page.d) * a.c.token_stride);
+  };
+  // this wave's part of a tile of K or V, to byte `to` of the ring
+  auto issue = [&](long long off, const char* base, unsigned in_run, int piece, int to) __attribute__((always_inline)) {
 #pragma unroll
-      for (int r = 0; r < ROUNDS; ++r) {
-        const int tok = min(ti * PA_TILE + RUN * r, (len - 1) & ~(RUN - 1));
-        const long long off = 2 * ((long long)__builtin_amdgcn_readlane(page, RUN * r) * a.c.page_stride +
-                                   (long long)(tok - quotient(a.c.page, tok) * a.c.page.d) * a.c.token_stride);
-        __builtin_amdgcn_global_load_lds((glb_cvoid*)(kp + off + k_lane), (lds_void*)&Kb[(4 * r + wave) * 64], 16, 0, 0);
-        __builtin_amdgcn_global_load_lds((glb_cvoid*)(vp + off + v_lane), (lds_void*)&Vb[(4 * r + wave) * 64], 16, 0, 0);
-      }
-    } else {
-      const int tc = min(t, len - 1);
-      const long long off = 2 * ((long long)page * a.c.page_stride + (long long)(tc - quotient(a.c.page, tc) * a.c.page.d) * a.c.token_stride);
-#pragma unroll
-      for (int r = 0; r < ROUNDS; ++r) {
-        const int lo = __shfl((int)(unsigned)off, RUN * r + ld_tok), hi = __shfl((int)(off >> 32), RUN * r + ld_tok);
-        const long long o = ((long long)hi << 32) | (unsigned)lo;
-        __builtin_amdgcn_global_load_lds((glb_cvoid*)(kp + o + 16 * ld_k), (lds_void*)&Kb[(4 * r + wave) * 64], 16, 0, 0);
-        __builtin_amdgcn_global_load_lds((glb_cvoid*)(vp + o + 16 * ld_v), (lds_void*)&Vb[(4 * r + wave) * 64], 16, 0, 0);
+    for (int r = 0; r < ROUNDS; ++r) {
+      const unsigned lds = ring_at + to + (NW * r + wave) * 1024;
+      if constexpr (RUNS) {
+        const int from = RUN * r + TPI * wave;
+        const unsigned lo = __builtin_amdgcn_readlane((int)(unsigned)off, from), hi = __builtin_amdgcn_readlane((int)(off >> 32), from);
+        load_to_lds(lds, base + (long long)((unsigned long long)hi << 32 | lo), in_run);
+      } else {
+        const unsigned lo = __shfl((int)(unsigned)off, RUN * r + ld_tok), hi = __shfl((int)(off >> 32), RUN * r + ld_tok);
+        load_to_lds(lds, base + (long long)((unsigned long long)hi << 32 | lo) + 16 * piece);
       }
     }
-    return valid;
   };
 
   // ---- query rows
-  x8 qf[RT][DS];
-  int limit[RT];
-  uint64_t anc[RT];
-#pragma unroll
-  for (int rt = 0; rt < RT; ++rt) {
-    const int r = row0 + wave * ROWS_W + 32 * rt + col;
-    const bool live = r < R;
-    const int tok = quotient(a.group, live ? r : row0), head = u.g * a.group.d + (live ? r - tok * a.group.d : 0);
-    limit[rt] = live ? sq.ctx + tok + 1 : 0;
-    anc[rt] = live && a.anc ? a.anc[sq.first + tok] : 0ull;
-    const T* qp = static_cast<const T*>(a.q) + (long long)(sq.first + tok) * a.q_tok + head * a.q_head + 8 * h;
+  x8 qf[DS];
+  const int my_row = row0 + 32 * wave + col;
+  const bool live = my_row < R;
+  const int my_tok = quotient(a.group, live ? my_row : row0);
+  const int limit = live ? sq.ctx + my_tok + 1 : 0;
+  const uint64_t anc = live && a.anc ? a.anc[sq.first + my_tok] : 0ull;
+  {
+    const int head = u.g * a.group.d + (live ? my_row - my_tok * a.group.d : 0);
+    const T* qp = static_cast<const T*>(a.q) + (long long)(sq.first + my_tok) * a.q_tok + head * a.q_head + 8 * h;
 #pragma unroll
     for (int j = 0; j < DS; ++j) {
       union { u32x4 u; x8 v; } c;
       c.u = u32x4{0, 0, 0, 0};
       if (live) c.u = *(const gvec*)(qp + 16 * j);
-      qf[rt][j] = c.v;
+      qf[j] = c.v;
     }
   }
-  floatx16 o[RT][DT];
-  float m_ref[RT], l_run[RT];
+  floatx16 o[DT];
+  float m_ref = -INFINITY, l_run = 0.f;
 #pragma unroll
-  for (int rt = 0; rt < RT; ++rt) {
-    m_ref[rt] = -INFINITY; l_run[rt] = 0.f;
+  for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
-    for (int dt = 0; dt < DT; ++dt)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) o[rt][dt][i] = 0.f;
-  }
-  // byte offsets of the operand reads inside a tile: K token col, piece 2j + h; V token 4h + (lane % 16) / 4, channels
-  // 16 * (lane / 16 % 2) + 4 * (lane % 4) of a tile of 32
-  int k_off[DS], v_off[DT];
-#pragma unroll
-  for (int j = 0; j < DS; ++j) k_off[j] = col * ROWB + (((2 * j + h) ^ swz_k(col)) << 4);
-  {
-    const int t = 4 * h + ((lane & 15) >> 2), c = 16 * ((lane >> 4) & 1) + 4 * (lane & 3);
-#pragma unroll
-    for (int dt = 0; dt < DT; ++dt) v_off[dt] = t * ROWB + (((4 * dt + (c >> 3)) ^ swz_v(t)) << 4) + ((c & 4) << 1);
-  }
+    for (int i = 0; i < 16; ++i) o[dt][i] = 0.f;
+  // Places of the operand reads inside a tile: K token col, piece 2j + h; V token 4h + (lane % 16) / 4, channels
+  // 16 * (lane / 16 % 2) + 4 * (lane % 4) of a tile of 32.  The swizzles touch other bits than what changes from read to read,
+  // or the same ones by exclusive or: one register each.
+  const int k_at = col * ROWB + ((swz_k(col) ^ h) << 4);
+  const int v_tok = 4 * h + ((lane & 15) >> 2), v_c = 16 * ((lane >> 4) & 1) + 4 * (lane & 3);
+  const int v_at = v_tok * ROWB + ((swz_v(v_tok) + (v_c >> 3)) << 4) + ((v_c & 4) << 1);
 
-  auto scores = [&](int hf, const char* kl, floatx16 (&s)[RT]) __attribute__((always_inline)) {
+  // Operands are read from the LDS four at a time, a group ahead of the matrix instructions that take them: a group is 128 cycles
+  // of the matrix unit, about what the LDS takes to answer.  (Vector instructions may move between.)
+#define PA_GROUP() __builtin_amdgcn_sched_barrier(0x406)
+  struct Four { x8 v[4]; };
+  auto read_k = [&](int g, int from) __attribute__((always_inline)) {      // group g of the tile's 2 DS operands of K
+    Four f;
+    const int base = from + k_at;
 #pragma unroll
-    for (int rt = 0; rt < RT; ++rt)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) s[rt][i] = 0.f;
-#pragma unroll
-    for (int j = 0; j < DS; ++j) {
-      const x8 kf = *reinterpret_cast<const x8*>(kl + 32 * hf * ROWB + k_off[j]);
-#pragma unroll
-      for (int rt = 0; rt < RT; ++rt) s[rt] = Elem<T>::mfma(kf, qf[rt][j], s[rt]);
-    }
+    for (int i = 0; i < 4; ++i) f.v[i] = *reinterpret_cast<const x8*>(ring + (base ^ ((2 * g + i / 2) << 5)) + 32 * (i & 1) * ROWB);
+    return f;
   };
-  auto mask = [&](uint32_t valid, int tok0, floatx16 (&s)[RT]) __attribute__((always_inline)) {
+  auto read_v = [&](int g, int from) __attribute__((always_inline)) {      // of its 4 DT operands of V
+    Four f;
+    const int base = from + v_at;
 #pragma unroll
-    for (int rt = 0; rt < RT; ++rt) {
-      const uint32_t b = (valid & (limit[rt] ? seen_bits(a, tok0, limit[rt], sq.ctx, anc[rt]) : 0u)) >> (4 * h);
-#pragma unroll
-      for (int i = 0; i < 16; ++i) if (!((b >> (8 * (i >> 2) + (i & 3))) & 1)) s[rt][i] = -INFINITY;
+    for (int i = 0; i < 4; ++i) {
+      const int n = 4 * g + i;
+      union { v4i16 q[2]; x8 v; } c;
+      const char* const rowp = ring + (base ^ ((n % DT) << 6)) + 16 * (n / DT) * ROWB;
+      c.q[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4i16*)(rowp));
+      c.q[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4i16*)(rowp + 8 * ROWB));
+      f.v[i] = c.v;
     }
+    return f;
   };
-  // the rows' references, raised where a score of the tile is too far above
-  auto refer = [&](const floatx16 (&s0)[RT], const floatx16 (&s1)[RT]) __attribute__((always_inline)) {
-    bool raise = false;
-    float mx[RT];
+  constexpr int KG = 2 * DS / 4, VG = 4 * DT / 4;
+  auto mask = [&](uint32_t valid, int tok0, floatx16& s) __attribute__((always_inline)) {
+    const uint32_t b = (valid & (limit ? seen_bits(a, tok0, limit, sq.ctx, anc) : 0u)) >> (4 * h);
 #pragma unroll
-    for (int rt = 0; rt < RT; ++rt) {
-      mx[rt] = fmaxf(s0[rt][0], s1[rt][0]);
+    for (int i = 0; i < 16; ++i) if (!((b >> (8 * (i >> 2) + (i & 3))) & 1)) s[i] = -INFINITY;
+  };
+  // the row's reference, raised where a score of the tile is too far above
+  auto refer = [&](const floatx16& s0, const floatx16& s1) __attribute__((always_inline)) {
+    float m = fmaxf(s0[0], s1[0]);
 #pragma unroll
-      for (int i = 1; i < 16; ++i) mx[rt] = fmaxf(mx[rt], fmaxf(s0[rt][i], s1[rt][i]));
-      mx[rt] *= a.scale_log2;
-      raise |= mx[rt] > m_ref[rt] + Elem<T>::SLACK;
+    for (int i = 1; i < 16; ++i) m = fmaxf(m, fmaxf(s0[i], s1[i]));
+    m *= a.scale_log2;
+    m = fmaxf(m, __shfl_xor(m, 32));
+    const float to = m > m_ref + Elem<T>::SLACK ? m - Elem<T>::SHIFT : m_ref;
+    const float f = to == m_ref ? 1.f : exp2f(m_ref - to);
+    m_ref = to;
+    l_run *= f;
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt) o[dt] *= f;
+  };
+  // numerators of half a tile, and their sum
+  auto soften = [&](const floatx16& s, x8 (&pf)[2]) __attribute__((always_inline)) {
+    const float ref = m_ref == -INFINITY ? 0.f : -m_ref;
+    float sum = 0.f;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      const float p = __builtin_amdgcn_exp2f(fmaf(s[i], a.scale_log2, ref));
+      sum += p;
+      pf[i >> 3][i & 7] = (T)p;
     }
-    if (__any(raise)) {
-#pragma unroll
-      for (int rt = 0; rt < RT; ++rt) {
-        const float m = fmaxf(mx[rt], __shfl_xor(mx[rt], 32));
-        if (m > m_ref[rt] + Elem<T>::SLACK) {
-          const float to = m - Elem<T>::SHIFT;
-          const float f = m_ref[rt] == -INFINITY ? 0.f : exp2f(m_ref[rt] - to);
-          m_ref[rt] = to;
-          l_run[rt] *= f;
-#pragma unroll
-          for (int dt = 0; dt < DT; ++dt) o[rt][dt] *= f;
+    return sum;
+  };
+  // NaN or Inf among values that not all rows see: a product with a numerator of 0 would be NaN, so they leave the tile, and the
+  // rows that see them are marked.  Every wave looks through what it has loaded itself.
+  auto sanitize = [&](int ti, unsigned long long valid, char* V) __attribute__((always_inline)) {
+#pragma unroll 1
+    for (int r = 0; r < ROUNDS; ++r) {
+      const int at = (NW * r + wave) * 64 + lane;
+      uint4* const q = reinterpret_cast<uint4*>(V) + at;
+      if (!any_nonfinite<T>(*q)) continue;
+      const int t = at / PPR, piece = (at % PPR) ^ swz_v(t), tok = ti * PA_TILE + t;
+      unsigned short* const e = reinterpret_cast<unsigned short*>(q);
+#pragma unroll 1
+      for (int k = 0; k < 8; ++k) {
+        const unsigned short x = e[k];
+        if ((x & Elem<T>::INF) != Elem<T>::INF) continue;
+        e[k] = 0;
+        if (!((valid >> t) & 1)) continue;
+        const int c = 8 * piece + k;
+        const unsigned kind = (x & 0x7fffu) != Elem<T>::INF ? 3u : x & 0x8000u ? 2u : 1u;
+#pragma unroll 1
+        for (int rl = 0; rl < ROWS && row0 + rl < R; ++rl) {
+          const int rt = quotient(a.group, row0 + rl);
+          const bool sees = a.anc ? tok < sq.ctx || ((a.anc[sq.first + rt] >> (tok - sq.ctx)) & 1) : tok <= sq.ctx + rt;
+          if (sees) atomicOr(&lost[rl][c / 16], kind << (2 * (c % 16)));
         }
+        any_lost = 1;
       }
     }
   };
-  auto soften = [&](const floatx16 (&s)[RT], x8 (&pf)[RT][2]) __attribute__((always_inline)) {
+  auto masked = [&](int ti, unsigned long long valid) __attribute__((always_inline)) { return valid != ~0ull || (ti + 1) * PA_TILE > open; };
+
+  for (int i = threadIdx.x; i < ROWS * (D / 16); i += PA_TILE_BLOCK) lost[i / (D / 16)][i % (D / 16)] = 0;
+  if (threadIdx.x == 0) any_lost = 0;
+  if (t_begin < t_end) {
+    // K(t) and V(t) lie in place t mod 3 of their halves of the ring.  In the exponentials' phase of tile t K(t+2) and V(t+1) are
+    // requested, into places that both groups of waves were done with a phase ago; they are waited for at the end of the
+    // matrix phase behind it, a phase or two before the first wave reads them.
+    int ti = t_begin, at = 0;                  // at: ring place of ti, in bytes
+    auto behind = [](int x) { return x == 2 * TILE_BYTES ? 0 : x + TILE_BYTES; };
+    constexpr int V0 = 3 * TILE_BYTES;
+    int page = look_up(ti), page_1 = look_up(ti + 1);
+    unsigned long long valid = present(ti, page), valid_next = 0;
+    long long off_1 = offset(ti, page);        // of tile t+1
+    issue(off_1, kp, k_lane, ld_k, 0);
+    issue(off_1, vp, v_lane, ld_v, V0);
+    if (ti + 1 < t_end) { valid_next = present(ti + 1, page_1); off_1 = offset(ti + 1, page_1); issue(off_1, kp, k_lane, ld_k, TILE_BYTES); }
+    int page_2 = look_up(ti + 2);
+    for (int i = threadIdx.x; i < TILE_BYTES / 16; i += PA_TILE_BLOCK) reinterpret_cast<uint4*>(ring + V0 + 2 * TILE_BYTES)[i] = make_uint4(0, 0, 0, 0);
+    __builtin_amdgcn_s_waitcnt(0x0F70);        // vmcnt(0)
+    __syncthreads();                           // (also: `lost` is cleared)
+    if (masked(ti, valid)) sanitize(ti, valid, ring + V0);
+    lds_barrier();
+    if (wave >= NW / 2) lds_barrier();         // the second group is a phase behind
+    x8 p[2][2];                                // (of the tile before the first: nothing)
 #pragma unroll
-    for (int rt = 0; rt < RT; ++rt) {
-      const float ref = m_ref[rt] == -INFINITY ? 0.f : -m_ref[rt];
+    for (int k = 0; k < 4; ++k)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) p[k >> 1][k & 1][i] = (T)0.f;
+    floatx16 s0, s1;
+    int v_before = 2 * TILE_BYTES;
+    while (true) {
+      // ---- matrix phase
+      Four now = read_v(0, V0 + v_before);
+#pragma unroll
+      for (int g = 0; g < VG; ++g) {
+        const Four next = g + 1 < VG ? read_v(g + 1, V0 + v_before) : read_k(0, at);
+        PA_GROUP();
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int n = 4 * g + i, ks = n / DT;
+          o[n % DT] = Elem<T>::mfma(now.v[i], p[ks >> 1][ks & 1], o[n % DT]);
+        }
+        PA_GROUP();
+        now = next;
+      }
+      if (ti == t_end) break;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) { s0[i] = 0.f; s1[i] = 0.f; }
+#pragma unroll
+      for (int g = 0; g < KG; ++g) {
+        Four next = now;
+        if (g + 1 < KG) next = read_k(g + 1, at);
+        PA_GROUP();
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          if (i & 1) s1 = Elem<T>::mfma(now.v[i], qf[2 * g + i / 2], s1);
+          else s0 = Elem<T>::mfma(now.v[i], qf[2 * g + i / 2], s0);
+        }
+        PA_GROUP();
+        now = next;
+      }
+      __builtin_amdgcn_s_waitcnt(0x0F70);
+      const bool mk = masked(ti, valid);
+      if (mk && ti > t_begin) sanitize(ti, valid, ring + V0 + at);
+      lds_barrier();
+      // ---- exponentials
+      const int at_1 = behind(at), at_2 = behind(at_1);
+      if (ti + 1 < t_end) issue(off_1, vp, v_lane, ld_v, V0 + at_1);
+      unsigned long long valid_2 = 0;
+      if (ti + 2 < t_end) { valid_2 = present(ti + 2, page_2); off_1 = offset(ti + 2, page_2); issue(off_1, kp, k_lane, ld_k, at_2); }
+      page_2 = look_up(ti + 3);
+      if (mk) { mask((uint32_t)valid, ti * PA_TILE, s0); mask((uint32_t)(valid >> 32), ti * PA_TILE + 32, s1); }
+      // Rows that have seen nothing so far need a reference first.  Scores far above one show in the sums (no maximum of all scores
+      // is needed for that): then once more with a new one.
+      bool raise = __any(m_ref == -INFINITY);
       float sum = 0.f;
-#pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        const float p = __builtin_amdgcn_exp2f(fmaf(s[rt][i], a.scale_log2, ref));
-        sum += p;
-        pf[rt][i >> 3][i & 7] = (T)p;
+#pragma unroll 1
+      for (int k = 0; k < 2; ++k) {
+        if (raise) refer(s0, s1);
+        sum = soften(s0, p[0]) + soften(s1, p[1]);
+        raise = __any(!(sum <= Elem<T>::MOST));
+        if (!raise) break;
       }
-      l_run[rt] += sum;
-    }
-  };
-  auto weigh = [&](int hf, const char* vl, const x8 (&pf)[RT][2]) __attribute__((always_inline)) {
-#pragma unroll
-    for (int ks = 0; ks < 2; ++ks)
-#pragma unroll
-      for (int dt = 0; dt < DT; ++dt) {
-        union { v4i16 q[2]; x8 v; } vf;
-        const char* const rowp = vl + (32 * hf + 16 * ks) * ROWB + v_off[dt];
-        vf.q[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4i16*)(rowp));
-        vf.q[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4i16*)(rowp + 8 * ROWB));
-#pragma unroll
-        for (int rt = 0; rt < RT; ++rt) o[rt][dt] = Elem<T>::mfma(vf.v, pf[rt][ks], o[rt][dt]);
-      }
-  };
-  auto compute = [&](int ti, unsigned long long valid, auto& Kb, auto& Vb) __attribute__((always_inline)) {
-    const char* const kl = reinterpret_cast<const char*>(&Kb[0]);
-    const char* const vl = reinterpret_cast<const char*>(&Vb[0]);
-    const int tok0 = ti * PA_TILE;
-    const bool masked = valid != ~0ull || tok0 + PA_TILE > open;
-    if (masked) {
-      // NaN or Inf among values that not all rows see: a product with a numerator of 0 would be NaN, so they leave the tile,
-      // and the rows that see them are marked.
-      for (int i = threadIdx.x; i < PA_TILE * PPR; i += PA_BLOCK) {
-        if (!any_nonfinite<T>(Vb[i])) continue;
-        const int t = i / PPR, piece = (i % PPR) ^ swz_v(t);
-        unsigned short* const e = reinterpret_cast<unsigned short*>(&Vb[i]);
-        for (int k = 0; k < 8; ++k) {
-          const unsigned short x = e[k];
-          if ((x & Elem<T>::INF) != Elem<T>::INF) continue;
-          e[k] = 0;
-          if (!((valid >> t) & 1)) continue;
-          const int c = 8 * piece + k;
-          const unsigned kind = (x & 0x7fffu) != Elem<T>::INF ? 3u : x & 0x8000u ? 2u : 1u;
-          for (int rl = 0; rl < ROWS && row0 + rl < R; ++rl) {
-            const int tok = quotient(a.group, row0 + rl);
-            const bool sees = a.anc ? tok0 + t < sq.ctx || ((a.anc[sq.first + tok] >> (tok0 + t - sq.ctx)) & 1) : tok0 + t <= sq.ctx + tok;
-            if (sees) atomicOr(&lost[rl][c / 16], kind << (2 * (c % 16)));
-          }
-          any_lost = 1;
-        }
-      }
+      l_run += sum;
+      valid = valid_next;
+      valid_next = valid_2;
+      v_before = at;
+      at = at_1;
+      ++ti;
       lds_barrier();
     }
-    floatx16 s0[RT], s1[RT];
-    x8 p0[RT][2], p1[RT][2];
-    scores(0, kl, s0);
-    scores(1, kl, s1);
-    if (masked) { mask((uint32_t)valid, tok0, s0); mask((uint32_t)(valid >> 32), tok0 + 32, s1); }
-    refer(s0, s1);
-    soften(s0, p0);
-    weigh(0, vl, p0);
-    soften(s1, p1);
-    weigh(1, vl, p1);
-  };
-
-  for (int i = threadIdx.x; i < ROWS * (D / 16); i += PA_BLOCK) lost[i / (D / 16)][i % (D / 16)] = 0;
-  if (threadIdx.x == 0) any_lost = 0;
-  int ti = t_begin, page = 0;
-  unsigned long long valid_a = 0, valid_b = 0;
-  if (ti < t_end) {
-    page = look_up(ti);
-    valid_a = issue(ti, page, kA, vA);
-    if (ti + 1 < t_end) page = look_up(ti + 1);
+    if (wave < NW / 2) lds_barrier();
   }
-  // One barrier per tile: every wave's part of it has landed, and everybody is done with the buffer that is filled next.
-  while (ti < t_end) {
-    __builtin_amdgcn_s_waitcnt(0x0F70);        // vmcnt(0)
-    lds_barrier();
-    if (ti + 1 < t_end) { valid_b = issue(ti + 1, page, kB, vB); if (ti + 2 < t_end) page = look_up(ti + 2); }
-    compute(ti, valid_a, kA, vA);
-    if (++ti >= t_end) break;
-    __builtin_amdgcn_s_waitcnt(0x0F70);
-    lds_barrier();
-    if (ti + 1 < t_end) { valid_a = issue(ti + 1, page, kA, vA); if (ti + 2 < t_end) page = look_up(ti + 2); }
-    compute(ti, valid_b, kB, vB);
-    ++ti;
-  }
-  __syncthreads();                             // the buffers become the output staging: an array per wave
-#pragma unroll
-  for (int rt = 0; rt < RT; ++rt) l_run[rt] += __shfl_xor(l_run[rt], 32);
-  uint4* const stage = wave == 0 ? kA : wave == 1 ? kB : wave == 2 ? vA : vB;
+  __syncthreads();                             // the ring becomes the output staging: a part per wave
+  l_run += __shfl_xor(l_run, 32);
   constexpr int QPR = D / 4, HALF = QPR / 2;   // 4-channel pieces of a row; they go through the LDS half a row at a time
+  uint4* const stage = reinterpret_cast<uint4*>(ring) + wave * 32 * HALF;
+  static_assert(NW * 32 * HALF * 16 <= 6 * TILE_BYTES, "the output staging fits the ring");
 #pragma unroll
-  for (int rt = 0; rt < RT; ++rt) {
-    const int rw = wave * ROWS_W + 32 * rt;
+  for (int half = 0; half < 2; ++half) {
+    wave_lds_fence();
 #pragma unroll
-    for (int half = 0; half < 2; ++half) {
-      wave_lds_fence();
+    for (int dt = 0; dt < DT / 2; ++dt)
 #pragma unroll
-      for (int dt = 0; dt < DT / 2; ++dt)
+      for (int k = 0; k < 4; ++k) {
+        union { floatx4 f; uint4 u; } c;
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          union { floatx4 f; uint4 u; } c;
-#pragma unroll
-          for (int i = 0; i < 4; ++i) c.f[i] = o[rt][half * (DT / 2) + dt][4 * k + i];
-          stage[col * HALF + ((8 * dt + 2 * k + h) ^ (col & 7))] = c.u;
-        }
-      wave_lds_fence();
-#pragma unroll 4
-      for (int i = lane; i < 32 * HALF; i += 64) {
-        const int rl = i / HALF, q = i % HALF, part = half * HALF + q, r = row0 + rw + rl;
-        const float M = __shfl(m_ref[rt], rl), L = __shfl(l_run[rt], rl);
-        if (r >= R) continue;
-        union { uint4 u; floatx4 f; } c;
-        c.u = stage[rl * HALF + (q ^ (rl & 7))];
-        const int tok = quotient(a.group, r), head = u.g * a.group.d + r - tok * a.group.d;
-        const long long row = sq.first + tok, slot = (long long)blockIdx.x * ROWS + rw + rl;
-        const unsigned gone = any_lost ? (lost[rw + rl][part / 4] >> (8 * (part % 4))) & 255u : 0u;
-        if (u.nparts == 1) {
-          write_row<T, D>(a, row, head, part, M, L, c.f, gone);
-        } else {
-          if (gone) {
-            unsigned* const b = reinterpret_cast<unsigned*>(&c.u);
-#pragma unroll
-            for (int k = 0; k < 4; ++k) if (const unsigned x = (gone >> (2 * k)) & 3) b[k] = x == 1 ? 0x7f800000u : x == 2 ? 0xff800000u : 0x7fc00000u;
-          }
-          *reinterpret_cast<uint4*>(&a.part_o[slot * D + 4 * part]) = c.u;
-          if (part == 0) { a.part_ml[2 * slot] = M; a.part_ml[2 * slot + 1] = L; }
-        }
-        if (a.splits && part == 0 && u.part == 0) a.row_parts[row * a.Hq + head] = make_int2((int)slot, u.nparts);
+        for (int i = 0; i < 4; ++i) c.f[i] = o[half * (DT / 2) + dt][4 * k + i];
+        stage[col * HALF + ((8 * dt + 2 * k + h) ^ (col & 7))] = c.u;
       }
+    wave_lds_fence();
+#pragma unroll 4
+    for (int i = lane; i < 32 * HALF; i += 64) {
+      const int rl = i / HALF, q = i % HALF, part = half * HALF + q, r = row0 + 32 * wave + rl;
+      const float M = __shfl(m_ref, rl), L = __shfl(l_run, rl);
+      if (r >= R) continue;
+      union { uint4 u; floatx4 f; } c;
+      c.u = stage[rl * HALF + (q ^ (rl & 7))];
+      const int tok = quotient(a.group, r), head = u.g * a.group.d + r - tok * a.group.d;
+      const long long row = sq.first + tok, slot = (long long)blockIdx.x * ROWS + 32 * wave + rl;
+      const unsigned gone = any_lost ? (lost[32 * wave + rl][part / 4] >> (8 * (part % 4))) & 255u : 0u;
+      if (u.nparts == 1) {
+        write_row<T, D>(a, row, head, part, M, L, c.f, gone);
+      } else {
+        if (gone) {
+          unsigned* const b = reinterpret_cast<unsigned*>(&c.u);
+#pragma unroll
+          for (int k = 0; k < 4; ++k) if (const unsigned x = (gone >> (2 * k)) & 3) b[k] = x == 1 ? 0x7f800000u : x == 2 ? 0xff800000u : 0x7fc00000u;
+        }
+        *reinterpret_cast<uint4*>(&a.part_o[slot * D + 4 * part]) = c.u;
+        if (part == 0) { a.part_ml[2 * slot] = M; a.part_ml[2 * slot + 1] = L; }
+      }
+      if (a.splits && part == 0 && u.part == 0) a.row_parts[row * a.Hq + head] = make_int2((int)slot, u.nparts);
     }
   }
 }
@@ -744,7 +795,7 @@ __global__ __launch_bounds__(PA_BLOCK) void paged_join_kernel(PagedAttnArgs a) {
   const int row = (int)(id / a.Hq), head = (int)(id % a.Hq);
   if (row < a.c.q_off[0] || row >= a.c.q_off[a.c.n_seqs]) return;       // padding
   const int2 rp = a.row_parts[id];
-  const long long apart = (long long)a.Hkv * a.block_rows;
+  const long long apart = (long long)(a.per_die ? 8 : a.Hkv) * a.block_rows;
   if (rp.y <= 1 || rp.x < 0 || rp.x + (rp.y - 1) * apart >= a.part_rows) return;
   constexpr int PIECES = D / 4, GROUPS = 64 / PIECES;                   // groups of lanes take every GROUPS-th part
   const int part = lane % PIECES, grp = lane / PIECES;
@@ -774,7 +825,7 @@ __global__ __launch_bounds__(PA_BLOCK) void paged_join_kernel(PagedAttnArgs a) {
 
 // How a call is cut up.
 struct Plan {
-  int rows;                  // per block: 16 and 32 wave-private, 128 tiles
+  int rows;                  // per block: 16 and 32 wave-private, 256 tiles
   long long grid;
   bool splits;
   size_t bytes;
@@ -782,11 +833,11 @@ struct Plan {
 Plan plan(const dsbd_paged_kv* c, int n_rows, int Hq, int Hkv, int D, PagedAttnArgs* a, void* workspace) {
   Plan p;
   const long long group = Hq / Hkv, most = (long long)std::min(c->max_new, n_rows) * group;     // rows of a sequence and KV head
-  p.rows = most <= 16 ? 16 : most <= 32 ? 32 : 128;
+  p.rows = most <= 16 ? 16 : most <= 32 ? 32 : PA_TILE_BLOCK / 2;
   const long long slots = p.rows <= 32 ? PA_SLOTS : PA_TILE_SLOTS;
   const long long units = ((long long)n_rows * group / p.rows + c->n_seqs) * Hkv;      // at most
   p.splits = units < 2 * slots;
-  p.grid = units + (p.splits ? slots : 0);
+  p.grid = units + (p.splits ? (slots + Hkv - 1) / Hkv * Hkv : 0);
   WorkspaceCarver w(workspace);
   float *po = nullptr, *ml = nullptr;
   int2* rp = nullptr;
@@ -799,6 +850,7 @@ Plan plan(const dsbd_paged_kv* c, int n_rows, int Hq, int Hkv, int D, PagedAttnA
   if (a) {
     a->splits = p.splits; a->part_o = po; a->part_ml = ml; a->row_parts = rp;
     a->part_rows = p.grid * p.rows; a->block_rows = p.rows;
+    a->per_die = Hkv % 8 == 0 ? (int)(p.grid / Hkv) : 0;
   }
   return p;
 }
@@ -843,8 +895,7 @@ extern "C" int32_t dsbd_paged_attention(const dsbd_paged_kv* cache, int32_t n_ro
   a.n_rows = n_rows; a.Hq = Hq; a.Hkv = Hkv; a.group = fast_div(Hq / Hkv); a.heads = fast_div(Hkv);
   a.scale_log2 = (float)((scale > 0.f ? (double)scale : 1.0 / sqrt((double)D)) * 1.4426950408889634);
   // (the tile kernel's short way adds a lane's place in a run of tokens as a 32-bit number of bytes)
-  a.page_run = cache->page_size % 32 == 0 ? 32 : cache->page_size % 16 == 0 ? 16 : cache->page_size % 8 == 0 ? 8 : 1;
-  if (cache->token_stride >= (1 << 25)) a.page_run = std::min(a.page_run, 8);
+  a.page_run = cache->page_size % 8 == 0 && cache->token_stride < (1 << 25) ? 8 : 1;
   a.fault = fault;
   hipStream_t stream = static_cast<hipStream_t>(stream_);
   const dim3 grid((unsigned)p.grid), block(PA_BLOCK);
@@ -853,7 +904,8 @@ extern "C" int32_t dsbd_paged_attention(const dsbd_paged_kv* cache, int32_t n_ro
   do {                                                                                                     \
     if (p.rows == 16) hipLaunchKernelGGL((paged_wave_kernel<T, DD, 1>), grid, block, 0, stream, a);        \
     else if (p.rows == 32) hipLaunchKernelGGL((paged_wave_kernel<T, DD, 2>), grid, block, 0, stream, a);   \
-    else hipLaunchKernelGGL((paged_tile_kernel<T, DD, 1>), grid, block, 0, stream, a);                     \
+    else if (a.page_run == 8) hipLaunchKernelGGL((paged_tile_kernel<T, DD, true>), grid, dim3(PA_TILE_BLOCK), 0, stream, a); \
+    else hipLaunchKernelGGL((paged_tile_kernel<T, DD, false>), grid, dim3(PA_TILE_BLOCK), 0, stream, a);    \
     DSBD_HIP_LAUNCH_CHECK();                                                                               \
     if (p.splits) hipLaunchKernelGGL((paged_join_kernel<T, DD>), join, block, 0, stream, a);               \
   } while (0)
