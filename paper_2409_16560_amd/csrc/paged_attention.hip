@@ -19,8 +19,7 @@ namespace {
 #define PA_STEP 32                 // tokens per wave step
 #define PA_SLOTS 512               // workgroups of the wave-private kernel that the device holds (70 KB of LDS each)
 #define PA_MIN_STEPS 4             // steps that a part has at least
-#define PA_TILE_BLOCK 512
-#define PA_TILE_SLOTS 256           // workgroups of the tile kernel that the device holds
+#define PA_TILE_SLOTS 512          // workgroups of 4 waves of the tile kernel that the device holds; half as many of 8
 
 typedef float floatx4 __attribute__((ext_vector_type(4)));
 typedef float floatx16 __attribute__((ext_vector_type(16)));
@@ -66,7 +65,6 @@ struct PagedAttnArgs {
   int2* row_parts;                             // [n_rows*Hq] first partial row, how many parts
   long long part_rows;                         // rows of part_o
   int block_rows;
-  int per_die;                                 // Hkv a multiple of 8: workgroups per KV head
   int32_t* fault;
 };
 
@@ -90,17 +88,10 @@ struct Unit { int s, g, rb, part, nparts; };
 template <int STEP>
 __device__ __forceinline__ bool find_unit(const PagedAttnArgs& a, int slots, Unit& u, int& part_steps) {
   const int lane = threadIdx.x & 63, rows = a.block_rows;
-  // Workgroups go to the 8 dies in turn: with 8 heads or a multiple a die takes its heads one after the other, so that what it has in
-  // hand shares the keys in its L2.
-  int at;
-  if (a.per_die) {
-    const int idx = blockIdx.x >> 3, k = idx / a.per_die;
-    u.g = (blockIdx.x & 7) + 8 * k;
-    at = idx - k * a.per_die;
-  } else {
-    at = quotient(a.heads, blockIdx.x);
-    u.g = blockIdx.x - at * a.Hkv;
-  }
+  // The head changes fastest: workgroups go to the 8 dies in turn, so that with 8 heads or a multiple what a die has in hand shares
+  // the keys in its L2.
+  const int at = quotient(a.heads, blockIdx.x);
+  u.g = blockIdx.x - at * a.Hkv;
   auto measure = [&](int s, int& nrb, int& steps) {
     nrb = 0; steps = 0;
     if (s < a.c.n_seqs) {
@@ -436,45 +427,36 @@ __global__ __launch_bounds__(PA_BLOCK) void paged_wave_kernel(PagedAttnArgs a) {
 
 // ---- tile kernel: many rows on the same keys
 //
-// Eight waves of 32 rows share tiles of 64 tokens of K and V in the LDS, a ring of three of each, filled by direct loads (no registers
-// in between); the pieces of a row are swizzled by the token, so that the operand reads, which go down the rows, spread over the
-// banks.  MFMA 32x32x16: S^T = K Q^T and O^T += V^T P^T as in the wave-private kernel; a lane owns a query row together with the
-// lane 32 further on, which has the other half of its tokens.
-// Two phases take turns: 32 matrix instructions (V of the tile before, K of this one) and the exponentials of a tile.  The waves
-// of a SIMD, w and w + 4, are always in different ones, with a barrier between phases: left to themselves they run in step,
-// both waiting for the matrix unit and then both for the vector unit.
+// Four or eight waves of 32 rows share tiles of 64 tokens of K and V in the LDS, two of each, filled by direct loads (no registers
+// in between) a tile ahead; the pieces of a row are swizzled by the token, so that the operand reads, which go down the rows,
+// spread over the banks.  MFMA 32x32x16: S^T = K Q^T and O^T += V^T P^T as in the wave-private kernel, a lane owns a query row
+// together with the lane 32 further on, which has the other half of its tokens.
 #define PA_TILE 64
 
-typedef __attribute__((address_space(3))) char lds_char;
+typedef __attribute__((address_space(3))) void lds_void;
+typedef const __attribute__((address_space(1))) void glb_cvoid;
 
 // Workgroup barrier that orders LDS traffic only (loads in flight stay in flight).
 __device__ __forceinline__ void lds_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
-// 16 bytes per lane from base + its offset to consecutive places in the LDS.  (Written out: behind the compiler's own form of
-// it every LDS read waits for all such loads, whatever part of the LDS they fill.  No register is written.)
-__device__ __forceinline__ void load_to_lds(unsigned lds, const char* base, unsigned lane_offset) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(lane_offset), "s"(base) : "memory");
-}
-__device__ __forceinline__ void load_to_lds(unsigned lds, const char* from) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds), "v"(from) : "memory");
-}
 
-// RUNS: pages are whole multiples of 8 tokens.
-template <typename T, int D, bool RUNS>
-__global__ __launch_bounds__(PA_TILE_BLOCK, 2) void paged_tile_kernel(PagedAttnArgs a) {
+// NW: waves, 4 where 128 rows hold all of a sequence's (two workgroups per CU), 8 above (one, which fills a tile for twice the rows):
+// 8 trees of 31 nodes with 4 heads per KV head on 8192 tokens 71 us against 88; a prompt of 8192 tokens, 32 heads of 128, 638 us
+// against 582; three chunks of 600 to 2100 tokens 247 us against 234.  RUNS: pages are whole multiples of 8 tokens.
+template <typename T, int D, int NW, bool RUNS>
+__global__ __launch_bounds__(64 * NW, 2) void paged_tile_kernel(PagedAttnArgs a) {
   typedef typename Elem<T>::x8 x8;
-  constexpr int NW = PA_TILE_BLOCK / 64, ROWS = 32 * NW;
   constexpr int DS = D / 16, DT = D / 32;               // k-steps of S^T, channel tiles of O^T
+  constexpr int BLOCK = 64 * NW, ROWS = 32 * NW;
   constexpr int PPR = D / 8, ROWB = 2 * D;              // 16-byte pieces and bytes of a row
-  constexpr int TPI = 64 / PPR, RUN = NW * TPI, ROUNDS = PA_TILE / RUN;      // tokens per load instruction, and of all waves; instructions per tile
-  constexpr int TILE_BYTES = PA_TILE * ROWB;
-  __shared__ __attribute__((aligned(16))) char ring[6 * TILE_BYTES];         // three tiles of K, three of V
+  constexpr int TPI = 64 / PPR, ROUNDS = PA_TILE / (NW * TPI);    // tokens per load instruction, instructions per wave and tile
+  __shared__ uint4 kA[PA_TILE * PPR], kB[PA_TILE * PPR], vA[PA_TILE * PPR], vB[PA_TILE * PPR];
   // two bits per row and channel whose sum is +Inf, -Inf or NaN (both)
   __shared__ unsigned lost[ROWS][D / 16];
   __shared__ int any_lost;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 31, h = lane >> 5;
   Unit u;
   int part_tiles;
-  if (!find_unit<PA_TILE>(a, PA_TILE_SLOTS, u, part_tiles)) return;
+  if (!find_unit<PA_TILE>(a, PA_TILE_SLOTS * 4 / NW, u, part_tiles)) return;
   const Seq sq = sequence(a, u.s);
   const int R = sq.n * a.group.d, row0 = u.rb * ROWS, len = sq.ctx + sq.n;
   if (u.g == 0 && u.rb == 0 && u.part == 0 && threadIdx.x == 0 && !sq.good) atomicOr(a.fault, DSBD_FAULT_BOUNDS);
@@ -492,12 +474,12 @@ __global__ __launch_bounds__(PA_TILE_BLOCK, 2) void paged_tile_kernel(PagedAttnA
   // swizzles: K is read down 16 tokens at one piece, V down 8 tokens at 4 pieces in a row
   auto swz_k = [](int t) { return D == 128 ? t & 15 : (t >> 1) & 7; };
   auto swz_v = [](int t) { return D == 128 ? 4 * (t & 3) : 4 * ((t >> 1) & 1); };
+  constexpr int RUN = NW * TPI;                // tokens per round of the waves
   const int ld_tok = TPI * wave + lane / PPR, ld_k = (lane % PPR) ^ swz_k(ld_tok), ld_v = (lane % PPR) ^ swz_v(ld_tok);
   static_assert(RUN % 16 == 0, "a round is a whole number of swizzle periods");
   const char* const kp = static_cast<const char*>(a.k_pages) + 2 * (long long)u.g * a.c.head_stride;
   const char* const vp = static_cast<const char*>(a.v_pages) + 2 * (long long)u.g * a.c.head_stride;
   const unsigned k_lane = (unsigned)(lane / PPR * 2 * (int)a.c.token_stride + 16 * ld_k), v_lane = (unsigned)(lane / PPR * 2 * (int)a.c.token_stride + 16 * ld_v);
-  const unsigned ring_at = (unsigned)(uintptr_t)(lds_char*)ring;
   // lane l: the page of token l of a tile
   auto look_up = [&](int ti) __attribute__((always_inline)) {
     const int p = quotient(a.c.page, min(ti * PA_TILE + lane, len - 1));
@@ -516,18 +498,22 @@ __global__ __launch_bounds__(PA_TILE_BLOCK, 2) void paged_tile_kernel(PagedAttnA
     page = page >= 0 && page < a.c.n_pages ? page : 0;
     return 2 * ((long long)page * a.c.page_stride + (long long)(t - quotient(a.c.page, t) * a.c.page.d) * a.c.token_stride);
   };
-  // this wave's part of a tile of K or V, to byte `to` of the ring
-  auto issue = [&](long long off, const char* base, unsigned in_run, int piece, int to) __attribute__((always_inline)) {
+  // this wave's part of a tile of K and V
+  auto issue = [&](int ti, int page, auto& Kb, auto& Vb) __attribute__((always_inline)) {
+    const long long off = offset(ti, page);
 #pragma unroll
     for (int r = 0; r < ROUNDS; ++r) {
-      const unsigned lds = ring_at + to + (NW * r + wave) * 1024;
       if constexpr (RUNS) {
         const int from = RUN * r + TPI * wave;
         const unsigned lo = __builtin_amdgcn_readlane((int)(unsigned)off, from), hi = __builtin_amdgcn_readlane((int)(off >> 32), from);
-        load_to_lds(lds, base + (long long)((unsigned long long)hi << 32 | lo), in_run);
+        const long long o = (long long)((unsigned long long)hi << 32 | lo);
+        __builtin_amdgcn_global_load_lds((glb_cvoid*)(kp + o + k_lane), (lds_void*)&Kb[(NW * r + wave) * 64], 16, 0, 0);
+        __builtin_amdgcn_global_load_lds((glb_cvoid*)(vp + o + v_lane), (lds_void*)&Vb[(NW * r + wave) * 64], 16, 0, 0);
       } else {
         const unsigned lo = __shfl((int)(unsigned)off, RUN * r + ld_tok), hi = __shfl((int)(off >> 32), RUN * r + ld_tok);
-        load_to_lds(lds, base + (long long)((unsigned long long)hi << 32 | lo) + 16 * piece);
+        const long long o = (long long)((unsigned long long)hi << 32 | lo);
+        __builtin_amdgcn_global_load_lds((glb_cvoid*)(kp + o + 16 * ld_k), (lds_void*)&Kb[(NW * r + wave) * 64], 16, 0, 0);
+        __builtin_amdgcn_global_load_lds((glb_cvoid*)(vp + o + 16 * ld_v), (lds_void*)&Vb[(NW * r + wave) * 64], 16, 0, 0);
       }
     }
   };
@@ -556,39 +542,40 @@ __global__ __launch_bounds__(PA_TILE_BLOCK, 2) void paged_tile_kernel(PagedAttnA
   for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
     for (int i = 0; i < 16; ++i) o[dt][i] = 0.f;
-  // Places of the operand reads inside a tile: K token col, piece 2j + h; V token 4h + (lane % 16) / 4, channels
-  // 16 * (lane / 16 % 2) + 4 * (lane % 4) of a tile of 32.  The swizzles touch other bits than what changes from read to read,
-  // or the same ones by exclusive or: one register each.
-  const int k_at = col * ROWB + ((swz_k(col) ^ h) << 4);
-  const int v_tok = 4 * h + ((lane & 15) >> 2), v_c = 16 * ((lane >> 4) & 1) + 4 * (lane & 3);
-  const int v_at = v_tok * ROWB + ((swz_v(v_tok) + (v_c >> 3)) << 4) + ((v_c & 4) << 1);
+  // byte offsets of the operand reads inside a tile: K token col, piece 2j + h; V token 4h + (lane % 16) / 4, channels
+  // 16 * (lane / 16 % 2) + 4 * (lane % 4) of a tile of 32
+  int k_off[DS], v_off[DT];
+#pragma unroll
+  for (int j = 0; j < DS; ++j) k_off[j] = col * ROWB + (((2 * j + h) ^ swz_k(col)) << 4);
+  {
+    const int t = 4 * h + ((lane & 15) >> 2), c = 16 * ((lane >> 4) & 1) + 4 * (lane & 3);
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt) v_off[dt] = t * ROWB + (((4 * dt + (c >> 3)) ^ swz_v(t)) << 4) + ((c & 4) << 1);
+  }
 
   // Operands are read from the LDS four at a time, a group ahead of the matrix instructions that take them: a group is 128 cycles
   // of the matrix unit, about what the LDS takes to answer.  (Vector instructions may move between.)
 #define PA_GROUP() __builtin_amdgcn_sched_barrier(0x406)
   struct Four { x8 v[4]; };
-  auto read_k = [&](int g, int from) __attribute__((always_inline)) {      // group g of the tile's 2 DS operands of K
+  auto read_k = [&](int g, const char* kl) __attribute__((always_inline)) {      // group g of the tile's 2 DS operands of K
     Four f;
-    const int base = from + k_at;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) f.v[i] = *reinterpret_cast<const x8*>(ring + (base ^ ((2 * g + i / 2) << 5)) + 32 * (i & 1) * ROWB);
+    for (int i = 0; i < 4; ++i) f.v[i] = *reinterpret_cast<const x8*>(kl + 32 * (4 * g / DS) * ROWB + k_off[(4 * g + i) % DS]);
     return f;
   };
-  auto read_v = [&](int g, int from) __attribute__((always_inline)) {      // of its 4 DT operands of V
+  auto read_v = [&](int g, const char* vl) __attribute__((always_inline)) {      // of its 4 DT operands of V
     Four f;
-    const int base = from + v_at;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const int n = 4 * g + i;
       union { v4i16 q[2]; x8 v; } c;
-      const char* const rowp = ring + (base ^ ((n % DT) << 6)) + 16 * (n / DT) * ROWB;
+      const char* const rowp = vl + 16 * (n / DT) * ROWB + v_off[n % DT];
       c.q[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4i16*)(rowp));
       c.q[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4i16*)(rowp + 8 * ROWB));
       f.v[i] = c.v;
     }
     return f;
   };
-  constexpr int KG = 2 * DS / 4, VG = 4 * DT / 4;
   auto mask = [&](uint32_t valid, int tok0, floatx16& s) __attribute__((always_inline)) {
     const uint32_t b = (valid & (limit ? seen_bits(a, tok0, limit, sq.ctx, anc) : 0u)) >> (4 * h);
 #pragma unroll
@@ -621,16 +608,12 @@ __global__ __launch_bounds__(PA_TILE_BLOCK, 2) void paged_tile_kernel(PagedAttnA
     return sum;
   };
   // NaN or Inf among values that not all rows see: a product with a numerator of 0 would be NaN, so they leave the tile, and the
-  // rows that see them are marked.  Every wave looks through what it has loaded itself.
-  auto sanitize = [&](int ti, unsigned long long valid, char* V) __attribute__((always_inline)) {
-#pragma unroll 1
-    for (int r = 0; r < ROUNDS; ++r) {
-      const int at = (NW * r + wave) * 64 + lane;
-      uint4* const q = reinterpret_cast<uint4*>(V) + at;
-      if (!any_nonfinite<T>(*q)) continue;
-      const int t = at / PPR, piece = (at % PPR) ^ swz_v(t), tok = ti * PA_TILE + t;
-      unsigned short* const e = reinterpret_cast<unsigned short*>(q);
-#pragma unroll 1
+  // rows that see them are marked.
+  auto sanitize = [&](int tok0, unsigned long long valid, auto& Vb) __attribute__((always_inline)) {
+    for (int i = threadIdx.x; i < PA_TILE * PPR; i += BLOCK) {
+      if (!any_nonfinite<T>(Vb[i])) continue;
+      const int t = i / PPR, piece = (i % PPR) ^ swz_v(t);
+      unsigned short* const e = reinterpret_cast<unsigned short*>(&Vb[i]);
       for (int k = 0; k < 8; ++k) {
         const unsigned short x = e[k];
         if ((x & Elem<T>::INF) != Elem<T>::INF) continue;
@@ -638,115 +621,100 @@ __global__ __launch_bounds__(PA_TILE_BLOCK, 2) void paged_tile_kernel(PagedAttnA
         if (!((valid >> t) & 1)) continue;
         const int c = 8 * piece + k;
         const unsigned kind = (x & 0x7fffu) != Elem<T>::INF ? 3u : x & 0x8000u ? 2u : 1u;
-#pragma unroll 1
         for (int rl = 0; rl < ROWS && row0 + rl < R; ++rl) {
-          const int rt = quotient(a.group, row0 + rl);
-          const bool sees = a.anc ? tok < sq.ctx || ((a.anc[sq.first + rt] >> (tok - sq.ctx)) & 1) : tok <= sq.ctx + rt;
+          const int tok = quotient(a.group, row0 + rl);
+          const bool sees = a.anc ? tok0 + t < sq.ctx || ((a.anc[sq.first + tok] >> (tok0 + t - sq.ctx)) & 1) : tok0 + t <= sq.ctx + tok;
           if (sees) atomicOr(&lost[rl][c / 16], kind << (2 * (c % 16)));
         }
         any_lost = 1;
       }
     }
-  };
-  auto masked = [&](int ti, unsigned long long valid) __attribute__((always_inline)) { return valid != ~0ull || (ti + 1) * PA_TILE > open; };
-
-  for (int i = threadIdx.x; i < ROWS * (D / 16); i += PA_TILE_BLOCK) lost[i / (D / 16)][i % (D / 16)] = 0;
-  if (threadIdx.x == 0) any_lost = 0;
-  if (t_begin < t_end) {
-    // K(t) and V(t) lie in place t mod 3 of their halves of the ring.  In the exponentials' phase of tile t K(t+2) and V(t+1) are
-    // requested, into places that both groups of waves were done with a phase ago; they are waited for at the end of the
-    // matrix phase behind it, a phase or two before the first wave reads them.
-    int ti = t_begin, at = 0;                  // at: ring place of ti, in bytes
-    auto behind = [](int x) { return x == 2 * TILE_BYTES ? 0 : x + TILE_BYTES; };
-    constexpr int V0 = 3 * TILE_BYTES;
-    int page = look_up(ti), page_1 = look_up(ti + 1);
-    unsigned long long valid = present(ti, page), valid_next = 0;
-    long long off_1 = offset(ti, page);        // of tile t+1
-    issue(off_1, kp, k_lane, ld_k, 0);
-    issue(off_1, vp, v_lane, ld_v, V0);
-    if (ti + 1 < t_end) { valid_next = present(ti + 1, page_1); off_1 = offset(ti + 1, page_1); issue(off_1, kp, k_lane, ld_k, TILE_BYTES); }
-    int page_2 = look_up(ti + 2);
-    for (int i = threadIdx.x; i < TILE_BYTES / 16; i += PA_TILE_BLOCK) reinterpret_cast<uint4*>(ring + V0 + 2 * TILE_BYTES)[i] = make_uint4(0, 0, 0, 0);
-    __builtin_amdgcn_s_waitcnt(0x0F70);        // vmcnt(0)
-    __syncthreads();                           // (also: `lost` is cleared)
-    if (masked(ti, valid)) sanitize(ti, valid, ring + V0);
     lds_barrier();
-    if (wave >= NW / 2) lds_barrier();         // the second group is a phase behind
-    x8 p[2][2];                                // (of the tile before the first: nothing)
+  };
+  auto compute = [&](int ti, unsigned long long valid, auto& Kb, auto& Vb) __attribute__((always_inline)) {
+    const char* const kl = reinterpret_cast<const char*>(&Kb[0]);
+    const char* const vl = reinterpret_cast<const char*>(&Vb[0]);
+    const int tok0 = ti * PA_TILE;
+    const bool masked = valid != ~0ull || tok0 + PA_TILE > open;
+    if (masked) sanitize(tok0, valid, Vb);
+    floatx16 s[2];
+    x8 p[2][2];
+    float sum = 0.f;
+    constexpr int KG = 2 * DS / 4, VG = 4 * DT / 4;
 #pragma unroll
-    for (int k = 0; k < 4; ++k)
+    for (int hf = 0; hf < 2; ++hf)
 #pragma unroll
-      for (int i = 0; i < 8; ++i) p[k >> 1][k & 1][i] = (T)0.f;
-    floatx16 s0, s1;
-    int v_before = 2 * TILE_BYTES;
-    while (true) {
-      // ---- matrix phase
-      Four now = read_v(0, V0 + v_before);
+      for (int i = 0; i < 16; ++i) s[hf][i] = 0.f;
+    Four now = read_k(0, kl);
 #pragma unroll
-      for (int g = 0; g < VG; ++g) {
-        const Four next = g + 1 < VG ? read_v(g + 1, V0 + v_before) : read_k(0, at);
-        PA_GROUP();
+    for (int g = 0; g < KG; ++g) {
+      const Four next = g + 1 < KG ? read_k(g + 1, kl) : read_v(0, vl);
+      PA_GROUP();
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int n = 4 * g + i, ks = n / DT;
-          o[n % DT] = Elem<T>::mfma(now.v[i], p[ks >> 1][ks & 1], o[n % DT]);
-        }
-        PA_GROUP();
-        now = next;
-      }
-      if (ti == t_end) break;
-#pragma unroll
-      for (int i = 0; i < 16; ++i) { s0[i] = 0.f; s1[i] = 0.f; }
-#pragma unroll
-      for (int g = 0; g < KG; ++g) {
-        Four next = now;
-        if (g + 1 < KG) next = read_k(g + 1, at);
-        PA_GROUP();
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          if (i & 1) s1 = Elem<T>::mfma(now.v[i], qf[2 * g + i / 2], s1);
-          else s0 = Elem<T>::mfma(now.v[i], qf[2 * g + i / 2], s0);
-        }
-        PA_GROUP();
-        now = next;
-      }
-      __builtin_amdgcn_s_waitcnt(0x0F70);
-      const bool mk = masked(ti, valid);
-      if (mk && ti > t_begin) sanitize(ti, valid, ring + V0 + at);
-      lds_barrier();
-      // ---- exponentials
-      const int at_1 = behind(at), at_2 = behind(at_1);
-      if (ti + 1 < t_end) issue(off_1, vp, v_lane, ld_v, V0 + at_1);
-      unsigned long long valid_2 = 0;
-      if (ti + 2 < t_end) { valid_2 = present(ti + 2, page_2); off_1 = offset(ti + 2, page_2); issue(off_1, kp, k_lane, ld_k, at_2); }
-      page_2 = look_up(ti + 3);
-      if (mk) { mask((uint32_t)valid, ti * PA_TILE, s0); mask((uint32_t)(valid >> 32), ti * PA_TILE + 32, s1); }
-      // Rows that have seen nothing so far need a reference first.  Scores far above one show in the sums (no maximum of all scores
-      // is needed for that): then once more with a new one.
-      bool raise = __any(m_ref == -INFINITY);
-      float sum = 0.f;
-#pragma unroll 1
-      for (int k = 0; k < 2; ++k) {
-        if (raise) refer(s0, s1);
-        sum = soften(s0, p[0]) + soften(s1, p[1]);
-        raise = __any(!(sum <= Elem<T>::MOST));
-        if (!raise) break;
-      }
-      l_run += sum;
-      valid = valid_next;
-      valid_next = valid_2;
-      v_before = at;
-      at = at_1;
-      ++ti;
-      lds_barrier();
+      for (int i = 0; i < 4; ++i) s[4 * g / DS] = Elem<T>::mfma(now.v[i], qf[(4 * g + i) % DS], s[4 * g / DS]);
+      PA_GROUP();
+      now = next;
     }
-    if (wave < NW / 2) lds_barrier();
+    if (masked) { mask((uint32_t)valid, tok0, s[0]); mask((uint32_t)(valid >> 32), tok0 + 32, s[1]); }
+    // Rows that have seen nothing so far need a reference first.  Scores far above one show in the sums (no maximum of all scores
+    // is needed for that): then once more with a new one.
+    bool raise = __any(m_ref == -INFINITY);
+#pragma unroll 1
+    for (int k = 0; k < 2; ++k) {
+      if (raise) refer(s[0], s[1]);
+      sum = soften(s[0], p[0]) + soften(s[1], p[1]);
+      raise = __any(!(sum <= Elem<T>::MOST));
+      if (!raise) break;
+    }
+    l_run += sum;
+#pragma unroll
+    for (int g = 0; g < VG; ++g) {
+      Four next = now;
+      if (g + 1 < VG) next = read_v(g + 1, vl);
+      PA_GROUP();
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int n = 4 * g + i, ks = n / DT;
+        o[n % DT] = Elem<T>::mfma(now.v[i], p[ks >> 1][ks & 1], o[n % DT]);
+      }
+      PA_GROUP();
+      now = next;
+    }
+  };
+  for (int i = threadIdx.x; i < ROWS * (D / 16); i += BLOCK) lost[i / (D / 16)][i % (D / 16)] = 0;
+  if (threadIdx.x == 0) any_lost = 0;
+  // One barrier per tile: every wave's part of it has landed, and everybody is done with the buffers that are filled next.
+  if (t_begin < t_end) {
+    int ti = t_begin;
+    int page = look_up(ti);
+    unsigned long long valid = present(ti, page), valid_next = 0;
+    issue(ti, page, kA, vA);
+    page = look_up(ti + 1);
+    auto tile = [&](auto& K, auto& K_next, auto& V, auto& V_next) __attribute__((always_inline)) {
+      __builtin_amdgcn_s_waitcnt(0x0F70);      // vmcnt(0)
+      lds_barrier();
+      if (ti + 1 < t_end) {
+        valid_next = present(ti + 1, page);
+        issue(ti + 1, page, K_next, V_next);
+        page = look_up(ti + 2);
+      }
+      compute(ti, valid, K, V);
+      valid = valid_next;
+      ++ti;
+    };
+    while (true) {
+      tile(kA, kB, vA, vB);
+      if (ti >= t_end) break;
+      tile(kB, kA, vB, vA);
+      if (ti >= t_end) break;
+    }
   }
-  __syncthreads();                             // the ring becomes the output staging: a part per wave
+  __syncthreads();                             // the buffers become the output staging: a part per wave
   l_run += __shfl_xor(l_run, 32);
   constexpr int QPR = D / 4, HALF = QPR / 2;   // 4-channel pieces of a row; they go through the LDS half a row at a time
-  uint4* const stage = reinterpret_cast<uint4*>(ring) + wave * 32 * HALF;
-  static_assert(NW * 32 * HALF * 16 <= 6 * TILE_BYTES, "the output staging fits the ring");
+  constexpr int PER = NW / 4;                  // waves per buffer
+  static_assert(PER * 32 * HALF <= PA_TILE * PPR, "the output staging fits the buffers");
+  uint4* const stage = (wave < PER ? kA : wave < 2 * PER ? kB : wave < 3 * PER ? vA : vB) + wave % PER * 32 * HALF;
 #pragma unroll
   for (int half = 0; half < 2; ++half) {
     wave_lds_fence();
@@ -795,7 +763,7 @@ __global__ __launch_bounds__(PA_BLOCK) void paged_join_kernel(PagedAttnArgs a) {
   const int row = (int)(id / a.Hq), head = (int)(id % a.Hq);
   if (row < a.c.q_off[0] || row >= a.c.q_off[a.c.n_seqs]) return;       // padding
   const int2 rp = a.row_parts[id];
-  const long long apart = (long long)(a.per_die ? 8 : a.Hkv) * a.block_rows;
+  const long long apart = (long long)a.Hkv * a.block_rows;
   if (rp.y <= 1 || rp.x < 0 || rp.x + (rp.y - 1) * apart >= a.part_rows) return;
   constexpr int PIECES = D / 4, GROUPS = 64 / PIECES;                   // groups of lanes take every GROUPS-th part
   const int part = lane % PIECES, grp = lane / PIECES;
@@ -825,7 +793,7 @@ __global__ __launch_bounds__(PA_BLOCK) void paged_join_kernel(PagedAttnArgs a) {
 
 // How a call is cut up.
 struct Plan {
-  int rows;                  // per block: 16 and 32 wave-private, 256 tiles
+  int rows;                  // per block: 16 and 32 wave-private kernel, 128 and 256 tile kernel
   long long grid;
   bool splits;
   size_t bytes;
@@ -833,8 +801,8 @@ struct Plan {
 Plan plan(const dsbd_paged_kv* c, int n_rows, int Hq, int Hkv, int D, PagedAttnArgs* a, void* workspace) {
   Plan p;
   const long long group = Hq / Hkv, most = (long long)std::min(c->max_new, n_rows) * group;     // rows of a sequence and KV head
-  p.rows = most <= 16 ? 16 : most <= 32 ? 32 : PA_TILE_BLOCK / 2;
-  const long long slots = p.rows <= 32 ? PA_SLOTS : PA_TILE_SLOTS;
+  p.rows = most <= 16 ? 16 : most <= 32 ? 32 : most <= 128 ? 128 : 256;
+  const long long slots = p.rows <= 32 ? PA_SLOTS : p.rows == 128 ? PA_TILE_SLOTS : PA_TILE_SLOTS / 2;
   const long long units = ((long long)n_rows * group / p.rows + c->n_seqs) * Hkv;      // at most
   p.splits = units < 2 * slots;
   p.grid = units + (p.splits ? (slots + Hkv - 1) / Hkv * Hkv : 0);
@@ -850,7 +818,6 @@ Plan plan(const dsbd_paged_kv* c, int n_rows, int Hq, int Hkv, int D, PagedAttnA
   if (a) {
     a->splits = p.splits; a->part_o = po; a->part_ml = ml; a->row_parts = rp;
     a->part_rows = p.grid * p.rows; a->block_rows = p.rows;
-    a->per_die = Hkv % 8 == 0 ? (int)(p.grid / Hkv) : 0;
   }
   return p;
 }
@@ -900,12 +867,17 @@ extern "C" int32_t dsbd_paged_attention(const dsbd_paged_kv* cache, int32_t n_ro
   hipStream_t stream = static_cast<hipStream_t>(stream_);
   const dim3 grid((unsigned)p.grid), block(PA_BLOCK);
   const dim3 join((unsigned)(((long long)n_rows * Hq + PA_BLOCK / 64 - 1) / (PA_BLOCK / 64)));
+#define PA_TILES(T, DD, NW)                                                                                \
+  do {                                                                                                     \
+    if (a.page_run == 8) hipLaunchKernelGGL((paged_tile_kernel<T, DD, NW, true>), grid, dim3(64 * NW), 0, stream, a); \
+    else hipLaunchKernelGGL((paged_tile_kernel<T, DD, NW, false>), grid, dim3(64 * NW), 0, stream, a);     \
+  } while (0)
 #define PA_ROWS(T, DD)                                                                                     \
   do {                                                                                                     \
     if (p.rows == 16) hipLaunchKernelGGL((paged_wave_kernel<T, DD, 1>), grid, block, 0, stream, a);        \
     else if (p.rows == 32) hipLaunchKernelGGL((paged_wave_kernel<T, DD, 2>), grid, block, 0, stream, a);   \
-    else if (a.page_run == 8) hipLaunchKernelGGL((paged_tile_kernel<T, DD, true>), grid, dim3(PA_TILE_BLOCK), 0, stream, a); \
-    else hipLaunchKernelGGL((paged_tile_kernel<T, DD, false>), grid, dim3(PA_TILE_BLOCK), 0, stream, a);    \
+    else if (p.rows == 128) PA_TILES(T, DD, 4);                                                            \
+    else PA_TILES(T, DD, 8);                                                                               \
     DSBD_HIP_LAUNCH_CHECK();                                                                               \
     if (p.splits) hipLaunchKernelGGL((paged_join_kernel<T, DD>), join, block, 0, stream, a);               \
   } while (0)
@@ -914,6 +886,7 @@ extern "C" int32_t dsbd_paged_attention(const dsbd_paged_kv* cache, int32_t n_ro
   else PA_TYPES(64);
 #undef PA_TYPES
 #undef PA_ROWS
+#undef PA_TILES
   DSBD_HIP_LAUNCH_CHECK();
   return DSBD_OK;
 }
