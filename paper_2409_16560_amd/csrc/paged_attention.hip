@@ -83,8 +83,9 @@ __device__ __forceinline__ Seq sequence(const PagedAttnArgs& a, int s) {
 struct Unit { int s, g, rb, part, nparts; };
 
 // Which unit, and which part of it, a workgroup has: lengths lie in device memory, so every wave works it out for itself, a
-// lane per sequence (64 at a time).  A part is `len` steps long, the same for all: an even share of all units' steps over
-// the workgroups that the device holds.  False: nothing to do.
+// lane per sequence (64 at a time).  A unit is cut into even parts of at most `len` steps, where len is the shortest, to within a
+// sixteenth, that makes no more parts than the device holds workgroups, so that all run at once and end together; units that
+// are more than half as many as that are cut at an even share of all steps.  False: nothing to do.
 template <int STEP>
 __device__ __forceinline__ bool find_unit(const PagedAttnArgs& a, int slots, Unit& u, int& part_steps) {
   const int lane = threadIdx.x & 63, rows = a.block_rows;
@@ -92,32 +93,43 @@ __device__ __forceinline__ bool find_unit(const PagedAttnArgs& a, int slots, Uni
   // the keys in its L2.
   const int at = quotient(a.heads, blockIdx.x);
   u.g = blockIdx.x - at * a.Hkv;
-  auto measure = [&](int s, int& nrb, int& steps) {
-    nrb = 0; steps = 0;
-    if (s < a.c.n_seqs) {
-      const Seq q = sequence(a, s);
+  int nrb, steps, have = -1;
+  auto measure = [&](int s0) {
+    if (s0 == have) return;
+    have = s0; nrb = 0; steps = 0;
+    if (s0 + lane < a.c.n_seqs) {
+      const Seq q = sequence(a, s0 + lane);
       nrb = (int)(((long long)q.n * a.group.d + rows - 1) / rows);
       steps = q.good ? (q.ctx + q.n + STEP - 1) / STEP : 1;
     }
   };
+  auto count = [&](int len) { return steps > len ? (int)((unsigned)(steps + len - 1) / (unsigned)len) : 1; };
   int len = 0x7fffffff;
   if (a.splits) {
-    double total = 0.0;
+    double total = 0.0, units = 0.0;
     for (int s0 = 0; s0 < a.c.n_seqs; s0 += 64) {
-      int nrb, steps;
-      measure(s0 + lane, nrb, steps);
+      measure(s0);
       total += (double)nrb * (double)steps;
+      units += (double)nrb;
     }
     total = wave_sum(total) * a.Hkv;
-    len = (int)fmin(ceil(total / slots), 1e9);
-    len = max(len, PA_MIN_STEPS);
+    units = wave_sum(units) * a.Hkv;
+    len = max((int)fmin(ceil(total / slots), 1e9), PA_MIN_STEPS);
+    if (2.0 * units <= slots) {
+      int hi = 2 * len;                        // enough: at most slots / 2 parts of that length, and one more for each unit
+      while (hi - len > max(len / 16, 1)) {    // (at least 2 apart: mid lies between them)
+        const int mid = (len + hi) / 2;
+        double parts = 0.0;
+        for (int s0 = 0; s0 < a.c.n_seqs; s0 += 64) { measure(s0); parts += (double)nrb * count(mid); }
+        if (wave_sum(parts) * a.Hkv <= slots) hi = mid; else len = mid;
+      }
+      len = hi;
+    }
   }
-  part_steps = len;
   long long base = 0;
   for (int s0 = 0; s0 < a.c.n_seqs; s0 += 64) {
-    int nrb, steps;
-    measure(s0 + lane, nrb, steps);
-    const int np = steps > len ? (steps + len - 1) / len : 1;
+    measure(s0);
+    const int np = count(len);
     int upto = nrb * np;                       // inclusive sum over the lanes
     const int mine = upto;
 #pragma unroll
@@ -128,11 +140,12 @@ __device__ __forceinline__ bool find_unit(const PagedAttnArgs& a, int slots, Uni
       const int l = (int)__ffsll((long long)m) - 1;
       u.s = s0 + l;
       u.nparts = __builtin_amdgcn_readlane(np, l);
+      part_steps = (int)((unsigned)(__builtin_amdgcn_readlane(steps, l) + u.nparts - 1) / (unsigned)u.nparts);
       const int rel = at - (int)__builtin_amdgcn_readlane((int)begin, l);
       const int n = __builtin_amdgcn_readlane(nrb, l), block = rel / u.nparts;
       u.part = rel - block * u.nparts;
       u.rb = n - 1 - block;                    // blocks that see most first
-      return true;
+      return block >= 0 && block < n;
     }
     base += __builtin_amdgcn_readlane(upto, 63);
   }
