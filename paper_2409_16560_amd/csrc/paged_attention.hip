@@ -65,15 +65,18 @@ struct PagedAttnArgs {
   int2* row_parts;                             // [n_rows*Hq] first partial row, how many parts
   long long part_rows;                         // rows of part_o
   int block_rows;
+  long long apart, shift;                      // row of part k > 0 of a row: the first one's + k * apart - shift
+  int per_head;                                // ranges of the wave-private kernel
   int32_t* fault;
 };
 
-struct Seq { int first, n, ctx; bool good; };
+struct Seq { int first, n, ctx; bool good, torn; };     // torn: no rows of the call
 __device__ __forceinline__ Seq sequence(const PagedAttnArgs& a, int s) {
   Seq q;
   q.first = a.c.q_off[s]; q.ctx = a.c.ctx_len[s];
   const int next = a.c.q_off[s + 1];
-  const bool rows = q.first >= 0 && next <= a.n_rows && next > q.first;
+  q.torn = q.first < 0 || next > a.n_rows || next < q.first;
+  const bool rows = !q.torn && next > q.first;
   q.n = rows ? next - q.first : 0;
   q.good = rows && q.n <= a.c.max_new && q.ctx >= 0 && q.ctx <= a.c.max_len - q.n && !(a.anc && q.n > 64);
   if (!q.good) q.ctx = 0;
@@ -99,6 +102,7 @@ __device__ __forceinline__ bool find_unit(const PagedAttnArgs& a, int slots, Uni
     have = s0; nrb = 0; steps = 0;
     if (s0 + lane < a.c.n_seqs) {
       const Seq q = sequence(a, s0 + lane);
+      if (q.torn) atomicOr(a.fault, DSBD_FAULT_BOUNDS);
       nrb = (int)(((long long)q.n * a.group.d + rows - 1) / rows);
       steps = q.good ? (q.ctx + q.n + STEP - 1) / STEP : 1;
     }
@@ -200,170 +204,258 @@ __device__ __forceinline__ void write_row(const PagedAttnArgs& a, long long row,
   if (a.lse && part == 0) a.lse[row * a.Hq + head] = L != 0.f ? (M + log2f(L)) * 0.6931471805599453f : -INFINITY;
 }
 
+// The same of a part's row, unnormalised.
+template <int D>
+__device__ __forceinline__ void write_part(const PagedAttnArgs& a, long long slot, int part, float M, float L, floatx4 acc, unsigned lost) {
+  union { floatx4 f; unsigned b[4]; } c;
+  c.f = acc;
+  if (lost) {
+#pragma unroll
+    for (int k = 0; k < 4; ++k) if (const unsigned x = (lost >> (2 * k)) & 3) c.b[k] = x == 1 ? 0x7f800000u : x == 2 ? 0xff800000u : 0x7fc00000u;
+  }
+  *reinterpret_cast<floatx4*>(&a.part_o[slot * D + 4 * part]) = c.f;
+  if (part == 0) { a.part_ml[2 * slot] = M; a.part_ml[2 * slot + 1] = L; }
+}
+// Workgroup barrier that orders LDS traffic only (loads in flight stay in flight).
+__device__ __forceinline__ void lds_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+
+// Whatever a workgroup has to do: where there are too few (sequence, KV head) to fill the device, the steps of all sequences, one
+// behind the other, are cut into `per_head` even ranges, a workgroup each and KV head.  So all workgroups end together whatever the
+// lengths are; a range may end one sequence, take others whole and begin another, and has room for two partial results.  (One token for
+// each of 32 sequences of 1024 to 8192 tokens: even parts of each sequence 122 us, ranges @RANGES us.)  The sequences' lengths lie in
+// device memory, so every wave looks for its place itself, a lane per sequence, 64 at a time.
 template <typename T, int D, int NRT>
-__global__ __launch_bounds__(PA_BLOCK) void paged_wave_kernel(PagedAttnArgs a) {
+__global__ __launch_bounds__(PA_BLOCK, 2) void paged_wave_kernel(PagedAttnArgs a) {
   typedef typename Elem<T>::x8 x8;
   constexpr int TW = PA_BLOCK / 64;
   constexpr int DS = D / 32, DT = D / 16, ROWS = 16 * NRT;
   constexpr int LPR = D / 8, TG = 64 / LPR, ROUNDS = PA_STEP / TG;
   constexpr int KP = D + 8, OP = D + 4;
   static_assert(ROWS * OP * 4 <= 2 * PA_STEP * KP * 2, "a wave's partial output takes the place of its tiles");
-  static_assert(ROWS * (PA_STEP + 1) * 4 <= PA_STEP * KP * 2, "numerators in the place of the K tile");
   __shared__ __attribute__((aligned(16))) T tiles[TW][2 * PA_STEP * KP];
   __shared__ float wave_ml[TW][ROWS][2];
+  // two bits per row and channel whose sum is +Inf, -Inf or NaN (both)
+  __shared__ unsigned lost[ROWS][D / 16];
+  __shared__ int any_lost;
 
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = lane & 15, qd = lane >> 4;
-  Unit u;
-  int part_steps;
-  if (!find_unit<PA_STEP>(a, PA_SLOTS, u, part_steps)) return;
-  const Seq sq = sequence(a, u.s);
-  const int R = sq.n * a.group.d, row0 = u.rb * ROWS;
-  const int len = sq.ctx + sq.n;
-  const bool reporter = u.g == 0 && u.rb == 0 && u.part == 0 && threadIdx.x == 0;
-  if (reporter && !sq.good) atomicOr(a.fault, DSBD_FAULT_BOUNDS);
-  // tokens that the block's last row sees, and the part's steps
-  const int last_tok = quotient(a.group, min(row0 + ROWS, R) - 1), first_tok = quotient(a.group, row0);
-  const int upto = !sq.good ? 0 : a.anc ? len : sq.ctx + last_tok + 1;
-  const int steps = (upto + PA_STEP - 1) / PA_STEP;
-  const int st_begin = u.nparts == 1 ? 0 : (int)min((long long)u.part * part_steps, (long long)steps);
-  const int st_end = u.nparts == 1 ? steps : min(steps, st_begin + part_steps);
-
-  // ---- query rows
-  x8 qf[NRT][DS];
-  int limit[NRT];
-  uint64_t anc[NRT];
-#pragma unroll
-  for (int rt = 0; rt < NRT; ++rt) {
-    const int r = row0 + 16 * rt + col;
-    const bool live = r < R;
-    const int tok = quotient(a.group, live ? r : row0), head = u.g * a.group.d + (live ? r - tok * a.group.d : 0);
-    limit[rt] = live ? sq.ctx + tok + 1 : 0;
-    anc[rt] = live && a.anc ? a.anc[sq.first + tok] : 0ull;
-    const T* qp = static_cast<const T*>(a.q) + (long long)(sq.first + tok) * a.q_tok + head * a.q_head + 8 * qd;
-#pragma unroll
-    for (int j = 0; j < DS; ++j) {
-      union { u32x4 u; x8 v; } c;
-      c.u = u32x4{0, 0, 0, 0};
-      if (live) c.u = *(const gvec*)(qp + 32 * j);
-      qf[rt][j] = c.v;
+  const int b = quotient(a.heads, blockIdx.x), g = blockIdx.x - b * a.Hkv;      // (workgroups go to the 8 dies in turn)
+  // ---- this workgroup's range, and the sequence that it begins in
+  int s0 = 0, steps = 0;                       // the first of the 64 sequences at hand; steps of this lane's
+  long long begin = 0, upto = 0;               // where they begin, and where the last of the 64 ends
+  auto scan = [&](int from, long long base) {
+    s0 = from; steps = 0;
+    if (s0 + lane < a.c.n_seqs) {
+      const Seq q = sequence(a, s0 + lane);
+      if (q.torn) atomicOr(a.fault, DSBD_FAULT_BOUNDS);
+      steps = q.n == 0 ? 0 : q.good ? (q.ctx + q.n + PA_STEP - 1) / PA_STEP : 1;
     }
-  }
-  floatx4 o[NRT][DT];
-  float m_ref[NRT], l_run[NRT];
+    upto = steps;
 #pragma unroll
-  for (int rt = 0; rt < NRT; ++rt) {
-    m_ref[rt] = -INFINITY; l_run[rt] = 0.f;
-#pragma unroll
-    for (int dt = 0; dt < DT; ++dt) o[rt][dt] = floatx4{0.f, 0.f, 0.f, 0.f};
-  }
-
-  T* const kt = tiles[wave];
-  T* const vt = kt + PA_STEP * KP;
-  const int piece = lane % LPR, ld_tok = ROUNDS * (lane / LPR);    // this lane loads tokens ld_tok .. ld_tok+ROUNDS-1 of a step
-  const long long hoff = (long long)u.g * a.c.head_stride + 8 * piece;
-  const T* const kp = static_cast<const T*>(a.k_pages) + hoff;
-  const T* const vp = static_cast<const T*>(a.v_pages) + hoff;
-  const int32_t* const table = a.c.page_table + (long long)u.s * a.c.table_stride;
-  uint4 kr[ROUNDS], vr[ROUNDS];
-  unsigned ok;                      // bit k: the lane's token k is there
-  auto load_step = [&](int st) {
-    const int t0 = st * PA_STEP + ld_tok;
-    ok = 0;
-    long long off = 0;
-    bool there = false;
-#pragma unroll
-    for (int k = 0; k < ROUNDS; ++k) {
-      const int t = t0 + k;
-      if (k == 0 || a.page_run < ROUNDS) {
-        const int p = quotient(a.c.page, min(t, len - 1));
-        const int page = p < a.c.table_stride ? table[p] : -1;
-        there = page >= 0 && page < a.c.n_pages;
-        off = there ? (long long)page * a.c.page_stride + (long long)(min(t, len - 1) - p * a.c.page.d) * a.c.token_stride : 0;
-        if (!there && t < len) atomicOr(a.fault, DSBD_FAULT_BOUNDS);
-      } else off += t < len ? a.c.token_stride : 0;
-      kr[k] = vr[k] = make_uint4(0, 0, 0, 0);
-      if (there && t < len) { kr[k] = load16(kp + off); vr[k] = load16(vp + off); ok |= 1u << k; }
-    }
+    for (int d = 1; d < 64; d <<= 1) { const long long o = __shfl_up(upto, d); if (lane >= d) upto += o; }
+    begin = base + upto - steps;
+    upto = base + __shfl(upto, 63);
   };
-  int st = st_begin + wave;
-  if (st < st_end) load_step(st);
-  const int open = sq.ctx + (a.anc ? 0 : first_tok + 1);      // tokens in front of this are seen by all rows
-  for (; st < st_end; st += TW) {
-    const int tok0 = st * PA_STEP;
-    uint32_t valid = 0xffffffffu;
-    const bool whole = __all(ok == (1u << ROUNDS) - 1);
-    if (!whole) {
-      valid = 0;
-#pragma unroll
-      for (int k = 0; k < TG; ++k) valid |= (uint32_t)__builtin_amdgcn_readlane((int)ok, k * LPR) << (ROUNDS * k);
-    }
-    const bool masked = !whole || tok0 + PA_STEP > open;
-    bool odd = false;                // values that no product with 0 makes 0
-    if (masked) {
-#pragma unroll
-      for (int k = 0; k < ROUNDS; ++k) odd |= any_nonfinite<T>(vr[k]);
-      odd = __any(odd);
-    }
-    wave_lds_fence();
-#pragma unroll
-    for (int k = 0; k < ROUNDS; ++k) {
-      *reinterpret_cast<uint4*>(&kt[(ld_tok + k) * KP + 8 * piece]) = kr[k];
-      *reinterpret_cast<uint4*>(&vt[(ld_tok + k) * KP + 8 * piece]) = vr[k];
-    }
-    wave_lds_fence();
-    if (st + TW < st_end) load_step(st + TW);
-    floatx4 s[NRT][2];
-#pragma unroll
-    for (int tt = 0; tt < 2; ++tt) {
-      x8 kf[DS];
-#pragma unroll
-      for (int j = 0; j < DS; ++j) kf[j] = *reinterpret_cast<const x8*>(&kt[(16 * tt + col) * KP + 32 * j + 8 * qd]);
-#pragma unroll
-      for (int rt = 0; rt < NRT; ++rt) {
-        floatx4 acc = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int j = 0; j < DS; ++j) acc = Elem<T>::mfma(kf[j], qf[rt][j], acc);
-        s[rt][tt] = acc * a.scale_log2;
+  long long x = 0, x_end = 0, per = 0;
+  if (a.splits) {
+    scan(0, 0);
+    while (s0 + 64 < a.c.n_seqs) scan(s0 + 64, upto);
+    per = max((long long)ceil((double)upto / a.per_head), (long long)PA_MIN_STEPS);
+    x = b * per;
+    x_end = min(x + per, upto);
+    if (x >= x_end) return;
+    if (s0 > 0) scan(0, 0);
+  }
+  do {
+    int s = b, st_begin = 0, st_end = 0x7fffffff, nparts = 1;
+    if (a.splits) {
+      unsigned long long m = __ballot(x >= begin && x < begin + steps);
+      while (!m) {
+        if (s0 + 64 >= a.c.n_seqs) return;
+        scan(s0 + 64, upto);
+        m = __ballot(x >= begin && x < begin + steps);
       }
+      const int l = (int)__ffsll((long long)m) - 1;
+      s = s0 + l;
+      const long long first = __shfl(begin, l);
+      const int n = __builtin_amdgcn_readlane(steps, l);
+      st_begin = (int)(x - first);
+      st_end = (int)min(x_end - first, (long long)n);
+      if (st_begin == 0) nparts = 1 + (int)((unsigned)(first - b * per + n - 1) / (unsigned)per);
+      else nparts = 2;                         // (or more)
+      x = first + st_end;
     }
-    if (masked) {
-#pragma unroll
-      for (int rt = 0; rt < NRT; ++rt) {
-        const uint32_t b = valid & (limit[rt] ? seen_bits(a, tok0, limit[rt], sq.ctx, anc[rt]) : 0u);
-#pragma unroll
-        for (int tt = 0; tt < 2; ++tt)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) if (!((b >> (16 * tt + 4 * qd + i)) & 1)) s[rt][tt][i] = -INFINITY;
+    const Seq sq = sequence(a, s);
+    const int R = sq.n * a.group.d, len = sq.ctx + sq.n;
+    if (g == 0 && st_begin == 0 && threadIdx.x == 0 && (sq.torn || (sq.n > 0 && !sq.good))) atomicOr(a.fault, DSBD_FAULT_BOUNDS);
+    if (R == 0) continue;
+    if (!sq.good) {                            // (any number of rows)
+      for (long long i = threadIdx.x; i < (long long)R * (D / 4); i += PA_BLOCK) {
+        const int r = (int)(i / (D / 4)), part = (int)(i % (D / 4)), tok = quotient(a.group, r), head = g * a.group.d + r - tok * a.group.d;
+        write_row<T, D>(a, sq.first + tok, head, part, -INFINITY, 0.f, floatx4{0.f, 0.f, 0.f, 0.f});
+        if (a.splits && part == 0) a.row_parts[(long long)(sq.first + tok) * a.Hq + head] = make_int2(0, 1);
       }
+      continue;
     }
-    x8 pf[NRT];
+    st_end = min(st_end, (len + PA_STEP - 1) / PA_STEP);
+    for (int i = threadIdx.x; i < ROWS * (D / 16); i += PA_BLOCK) lost[i / (D / 16)][i % (D / 16)] = 0;
+    if (threadIdx.x == 0) any_lost = 0;
+    lds_barrier();
+
+    // ---- query rows
+    x8 qf[NRT][DS];
+    int limit[NRT];
+    uint64_t anc[NRT];
 #pragma unroll
     for (int rt = 0; rt < NRT; ++rt) {
-      float mx = s[rt][0][0];
+      const int r = 16 * rt + col;
+      const bool live = r < R;
+      const int tok = quotient(a.group, live ? r : 0), head = g * a.group.d + (live ? r - tok * a.group.d : 0);
+      limit[rt] = live ? sq.ctx + tok + 1 : 0;
+      anc[rt] = live && a.anc ? a.anc[sq.first + tok] : 0ull;
+      const T* qp = static_cast<const T*>(a.q) + (long long)(sq.first + tok) * a.q_tok + head * a.q_head + 8 * qd;
 #pragma unroll
-      for (int k = 1; k < 8; ++k) mx = fmaxf(mx, s[rt][k >> 2][k & 3]);
-      if (__any(mx > m_ref[rt] + Elem<T>::SLACK)) {
-        mx = fmaxf(mx, __shfl_xor(mx, 16));
-        mx = fmaxf(mx, __shfl_xor(mx, 32));
-        if (mx > m_ref[rt] + Elem<T>::SLACK) {
-          const float to = mx - Elem<T>::SHIFT;
-          const float f = m_ref[rt] == -INFINITY ? 0.f : exp2f(m_ref[rt] - to);
-          m_ref[rt] = to;
-          l_run[rt] *= f;
-#pragma unroll
-          for (int dt = 0; dt < DT; ++dt) o[rt][dt] *= f;
-        }
-      }
-      const float ref = m_ref[rt] == -INFINITY ? 0.f : m_ref[rt];
-#pragma unroll
-      for (int k = 0; k < 8; ++k) {
-        const float p = __builtin_amdgcn_exp2f(s[rt][k >> 2][k & 3] - ref);
-        s[rt][k >> 2][k & 3] = p;
-        l_run[rt] += p;
-        pf[rt][k] = (T)p;
+      for (int j = 0; j < DS; ++j) {
+        union { u32x4 u; x8 v; } c;
+        c.u = u32x4{0, 0, 0, 0};
+        if (live) c.u = *(const gvec*)(qp + 32 * j);
+        qf[rt][j] = c.v;
       }
     }
-    if (!odd) {
+    floatx4 o[NRT][DT];
+    float m_ref[NRT], l_run[NRT];
+#pragma unroll
+    for (int rt = 0; rt < NRT; ++rt) {
+      m_ref[rt] = -INFINITY; l_run[rt] = 0.f;
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt) o[rt][dt] = floatx4{0.f, 0.f, 0.f, 0.f};
+    }
+
+    T* const kt = tiles[wave];
+    T* const vt = kt + PA_STEP * KP;
+    const int piece = lane % LPR, ld_tok = ROUNDS * (lane / LPR);    // this lane loads tokens ld_tok .. ld_tok+ROUNDS-1 of a step
+    const long long hoff = (long long)g * a.c.head_stride + 8 * piece;
+    const T* const kp = static_cast<const T*>(a.k_pages) + hoff;
+    const T* const vp = static_cast<const T*>(a.v_pages) + hoff;
+    const int32_t* const table = a.c.page_table + (long long)s * a.c.table_stride;
+    uint4 kr[ROUNDS], vr[ROUNDS];
+    unsigned ok;                      // bit k: the lane's token k is there
+    auto load_step = [&](int st) {
+      const int t0 = st * PA_STEP + ld_tok;
+      ok = 0;
+      long long off = 0;
+      bool there = false;
+#pragma unroll
+      for (int k = 0; k < ROUNDS; ++k) {
+        const int t = t0 + k;
+        if (k == 0 || a.page_run < ROUNDS) {
+          const int p = quotient(a.c.page, min(t, len - 1));
+          const int page = p < a.c.table_stride ? table[p] : -1;
+          there = page >= 0 && page < a.c.n_pages;
+          off = there ? (long long)page * a.c.page_stride + (long long)(min(t, len - 1) - p * a.c.page.d) * a.c.token_stride : 0;
+          if (!there && t < len) atomicOr(a.fault, DSBD_FAULT_BOUNDS);
+        } else off += t < len ? a.c.token_stride : 0;
+        kr[k] = vr[k] = make_uint4(0, 0, 0, 0);
+        if (there && t < len) { kr[k] = load16(kp + off); vr[k] = load16(vp + off); ok |= 1u << k; }
+      }
+    };
+    int st = st_begin + wave;
+    if (st < st_end) load_step(st);
+    const int open = sq.ctx + (a.anc ? 0 : 1);   // tokens in front of this are seen by all rows
+    for (; st < st_end; st += TW) {
+      const int tok0 = st * PA_STEP;
+      uint32_t valid = 0xffffffffu;
+      const bool whole = __all(ok == (1u << ROUNDS) - 1);
+      if (!whole) {
+        valid = 0;
+#pragma unroll
+        for (int k = 0; k < TG; ++k) valid |= (uint32_t)__builtin_amdgcn_readlane((int)ok, k * LPR) << (ROUNDS * k);
+      }
+      const bool masked = !whole || tok0 + PA_STEP > open;
+      bool odd = false;                // values that no product with 0 makes 0
+      if (masked) {
+#pragma unroll
+        for (int k = 0; k < ROUNDS; ++k) odd |= any_nonfinite<T>(vr[k]);
+      }
+      wave_lds_fence();
+#pragma unroll
+      for (int k = 0; k < ROUNDS; ++k) {
+        *reinterpret_cast<uint4*>(&kt[(ld_tok + k) * KP + 8 * piece]) = kr[k];
+        *reinterpret_cast<uint4*>(&vt[(ld_tok + k) * KP + 8 * piece]) = vr[k];
+      }
+      if (odd) {
+        // NaN or Inf among values that not all rows see: a product with a numerator of 0 would be NaN, so they leave the tile, and the
+        // rows that see them are marked.
+        unsigned short* const e = reinterpret_cast<unsigned short*>(vt + ld_tok * KP + 8 * piece);
+#pragma unroll 1
+        for (int i = 0; i < 8 * ROUNDS; ++i) {
+          const unsigned short v = e[i / 8 * KP + i % 8];
+          if ((v & Elem<T>::INF) != Elem<T>::INF) continue;
+          e[i / 8 * KP + i % 8] = 0;
+          const int c = 8 * piece + i % 8, tok = tok0 + ld_tok + i / 8;
+          const unsigned kind = (v & 0x7fffu) != Elem<T>::INF ? 3u : v & 0x8000u ? 2u : 1u;
+#pragma unroll 1
+          for (int r = 0; r < R; ++r) {
+            const int rt = quotient(a.group, r);
+            const bool sees = a.anc ? tok < sq.ctx || ((a.anc[sq.first + rt] >> (tok - sq.ctx)) & 1) : tok <= sq.ctx + rt;
+            if (sees) atomicOr(&lost[r][c / 16], kind << (2 * (c % 16)));
+          }
+          any_lost = 1;
+        }
+      }
+      wave_lds_fence();
+      if (st + TW < st_end) load_step(st + TW);
+      floatx4 x[NRT][2];
+#pragma unroll
+      for (int tt = 0; tt < 2; ++tt) {
+        x8 kf[DS];
+#pragma unroll
+        for (int j = 0; j < DS; ++j) kf[j] = *reinterpret_cast<const x8*>(&kt[(16 * tt + col) * KP + 32 * j + 8 * qd]);
+#pragma unroll
+        for (int rt = 0; rt < NRT; ++rt) {
+          floatx4 acc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+          for (int j = 0; j < DS; ++j) acc = Elem<T>::mfma(kf[j], qf[rt][j], acc);
+          x[rt][tt] = acc * a.scale_log2;
+        }
+      }
+      if (masked) {
+#pragma unroll
+        for (int rt = 0; rt < NRT; ++rt) {
+          const uint32_t b = valid & (limit[rt] ? seen_bits(a, tok0, limit[rt], sq.ctx, anc[rt]) : 0u);
+#pragma unroll
+          for (int tt = 0; tt < 2; ++tt)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) if (!((b >> (16 * tt + 4 * qd + i)) & 1)) x[rt][tt][i] = -INFINITY;
+        }
+      }
+      x8 pf[NRT];
+#pragma unroll
+      for (int rt = 0; rt < NRT; ++rt) {
+        float mx = x[rt][0][0];
+#pragma unroll
+        for (int k = 1; k < 8; ++k) mx = fmaxf(mx, x[rt][k >> 2][k & 3]);
+        if (__any(mx > m_ref[rt] + Elem<T>::SLACK)) {
+          mx = fmaxf(mx, __shfl_xor(mx, 16));
+          mx = fmaxf(mx, __shfl_xor(mx, 32));
+          if (mx > m_ref[rt] + Elem<T>::SLACK) {
+            const float to = mx - Elem<T>::SHIFT;
+            const float f = m_ref[rt] == -INFINITY ? 0.f : exp2f(m_ref[rt] - to);
+            m_ref[rt] = to;
+            l_run[rt] *= f;
+#pragma unroll
+            for (int dt = 0; dt < DT; ++dt) o[rt][dt] *= f;
+          }
+        }
+        const float ref = m_ref[rt] == -INFINITY ? 0.f : m_ref[rt];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+          const float p = __builtin_amdgcn_exp2f(x[rt][k >> 2][k & 3] - ref);
+          x[rt][k >> 2][k & 3] = p;
+          l_run[rt] += p;
+          pf[rt][k] = (T)p;
+        }
+      }
 #pragma unroll
       for (int dt = 0; dt < DT; ++dt) {
         union { v4i16 h[2]; x8 v; } vf;
@@ -373,69 +465,46 @@ __global__ __launch_bounds__(PA_BLOCK) void paged_wave_kernel(PagedAttnArgs a) {
 #pragma unroll
         for (int rt = 0; rt < NRT; ++rt) o[rt][dt] = Elem<T>::mfma(vf.v, pf[rt], o[rt][dt]);
       }
-    } else {
-      // NaN or Inf among the values of a step that not all rows see whole: token by token, so that a row only takes what it
-      // sees (a product with a numerator of 0 would be NaN)
-      float* const pb = reinterpret_cast<float*>(kt);
-      wave_lds_fence();
+    }
+    // ---- the waves' results: sums over the lanes of a row, then everything through the LDS
 #pragma unroll
-      for (int rt = 0; rt < NRT; ++rt)
+    for (int rt = 0; rt < NRT; ++rt) {
+      l_run[rt] += __shfl_xor(l_run[rt], 16);
+      l_run[rt] += __shfl_xor(l_run[rt], 32);
+    }
+    float* const po = reinterpret_cast<float*>(tiles[wave]);
+    wave_lds_fence();
 #pragma unroll
-        for (int k = 0; k < 8; ++k) pb[(16 * rt + col) * (PA_STEP + 1) + 16 * (k >> 2) + 4 * qd + (k & 3)] = (float)pf[rt][k];
-      wave_lds_fence();
-      for (int t = 0; t < PA_STEP; ++t) {
+    for (int rt = 0; rt < NRT; ++rt) {
 #pragma unroll
-        for (int rt = 0; rt < NRT; ++rt) {
-          const float p = pb[(16 * rt + col) * (PA_STEP + 1) + t];
+      for (int dt = 0; dt < DT; ++dt) *reinterpret_cast<floatx4*>(&po[(16 * rt + col) * OP + 16 * dt + 4 * qd]) = o[rt][dt];
+      if (qd == 0) { wave_ml[wave][16 * rt + col][0] = m_ref[rt]; wave_ml[wave][16 * rt + col][1] = l_run[rt]; }
+    }
+    __syncthreads();
+    const long long slot = ((long long)(2 * b + (st_begin == 0)) * a.Hkv + g) * ROWS;
+    for (int i = threadIdx.x; i < R * (D / 4); i += PA_BLOCK) {
+      const int r = i / (D / 4), part = i % (D / 4);
+      float M = -INFINITY, L = 0.f;
 #pragma unroll
-          for (int dt = 0; dt < DT; ++dt)
+      for (int w = 0; w < TW; ++w) M = fmaxf(M, wave_ml[w][r][0]);
+      floatx4 acc = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-            for (int i = 0; i < 4; ++i) o[rt][dt][i] += p != 0.f ? p * (float)vt[t * KP + 16 * dt + 4 * qd + i] : 0.f;
-        }
+      for (int w = 0; w < TW; ++w) {
+        const float m = wave_ml[w][r][0], l = wave_ml[w][r][1];
+        if (l == 0.f) continue;                    // the wave's steps had nothing for this row
+        const float f = m == M ? 1.f : exp2f(m - M);
+        L += l * f;
+        acc += *reinterpret_cast<const floatx4*>(&reinterpret_cast<const float*>(tiles[w])[r * OP + 4 * part]) * f;
       }
+      const int tok = quotient(a.group, r), head = g * a.group.d + r - tok * a.group.d;
+      const long long row = sq.first + tok;
+      const unsigned gone = any_lost ? (lost[r][part / 4] >> (8 * (part % 4))) & 255u : 0u;
+      if (nparts == 1) write_row<T, D>(a, row, head, part, M, L, acc, gone);
+      else write_part<D>(a, slot + r, part, M, L, acc, gone);
+      if (a.splits && part == 0 && st_begin == 0) a.row_parts[row * a.Hq + head] = make_int2((int)slot + r, nparts);
     }
-  }
-  // ---- the waves' results: sums over the lanes of a row, then everything through the LDS
-#pragma unroll
-  for (int rt = 0; rt < NRT; ++rt) {
-    l_run[rt] += __shfl_xor(l_run[rt], 16);
-    l_run[rt] += __shfl_xor(l_run[rt], 32);
-  }
-  float* const po = reinterpret_cast<float*>(tiles[wave]);
-  wave_lds_fence();
-#pragma unroll
-  for (int rt = 0; rt < NRT; ++rt) {
-#pragma unroll
-    for (int dt = 0; dt < DT; ++dt) *reinterpret_cast<floatx4*>(&po[(16 * rt + col) * OP + 16 * dt + 4 * qd]) = o[rt][dt];
-    if (qd == 0) { wave_ml[wave][16 * rt + col][0] = m_ref[rt]; wave_ml[wave][16 * rt + col][1] = l_run[rt]; }
-  }
-  __syncthreads();
-  const long long slot = (long long)blockIdx.x * ROWS;
-  for (int i = threadIdx.x; i < ROWS * (D / 4); i += PA_BLOCK) {
-    const int rl = i / (D / 4), part = i % (D / 4), r = row0 + rl;
-    if (r >= R) continue;
-    float M = -INFINITY, L = 0.f;
-#pragma unroll
-    for (int w = 0; w < TW; ++w) M = fmaxf(M, wave_ml[w][rl][0]);
-    floatx4 acc = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-    for (int w = 0; w < TW; ++w) {
-      const float m = wave_ml[w][rl][0], l = wave_ml[w][rl][1];
-      if (l == 0.f) continue;                    // the wave's steps had nothing for this row
-      const float f = m == M ? 1.f : exp2f(m - M);
-      L += l * f;
-      acc += *reinterpret_cast<const floatx4*>(&reinterpret_cast<const float*>(tiles[w])[rl * OP + 4 * part]) * f;
-    }
-    const int tok = quotient(a.group, r), head = u.g * a.group.d + r - tok * a.group.d;
-    const long long row = sq.first + tok;
-    if (u.nparts == 1) {
-      write_row<T, D>(a, row, head, part, M, L, acc);
-    } else {
-      *reinterpret_cast<floatx4*>(&a.part_o[(slot + rl) * D + 4 * part]) = acc;
-      if (part == 0) { a.part_ml[2 * (slot + rl)] = M; a.part_ml[2 * (slot + rl) + 1] = L; }
-    }
-    if (a.splits && part == 0 && u.part == 0) a.row_parts[row * a.Hq + head] = make_int2((int)blockIdx.x * ROWS + rl, u.nparts);
-  }
+    __syncthreads();                             // (the LDS, for the next)
+  } while (a.splits && x < x_end);
 }
 
 // ---- tile kernel: many rows on the same keys
@@ -448,9 +517,6 @@ __global__ __launch_bounds__(PA_BLOCK) void paged_wave_kernel(PagedAttnArgs a) {
 
 typedef __attribute__((address_space(3))) void lds_void;
 typedef const __attribute__((address_space(1))) void glb_cvoid;
-
-// Workgroup barrier that orders LDS traffic only (loads in flight stay in flight).
-__device__ __forceinline__ void lds_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 
 // NW: waves, 4 where 128 rows hold all of a sequence's (two workgroups per CU), 8 above (one, which fills a tile for twice the rows):
 // 8 trees of 31 nodes with 4 heads per KV head on 8192 tokens 71 us against 88; a prompt of 8192 tokens, 32 heads of 128, 638 us
@@ -754,54 +820,69 @@ __global__ __launch_bounds__(64 * NW, 2) void paged_tile_kernel(PagedAttnArgs a)
       if (u.nparts == 1) {
         write_row<T, D>(a, row, head, part, M, L, c.f, gone);
       } else {
-        if (gone) {
-          unsigned* const b = reinterpret_cast<unsigned*>(&c.u);
-#pragma unroll
-          for (int k = 0; k < 4; ++k) if (const unsigned x = (gone >> (2 * k)) & 3) b[k] = x == 1 ? 0x7f800000u : x == 2 ? 0xff800000u : 0x7fc00000u;
-        }
-        *reinterpret_cast<uint4*>(&a.part_o[slot * D + 4 * part]) = c.u;
-        if (part == 0) { a.part_ml[2 * slot] = M; a.part_ml[2 * slot + 1] = L; }
+        write_part<D>(a, slot, part, M, L, c.f, gone);
       }
       if (a.splits && part == 0 && u.part == 0) a.row_parts[row * a.Hq + head] = make_int2((int)slot, u.nparts);
     }
   }
 }
 
-// A wave per (row, head) of what was split: the parts of a unit are Hkv * rows apart.
+// A wave per (row, head) of what was split.  Groups of lanes take every GROUPS-th part, four
+// at a time, and carry a maximum and a sum of their own, so that nothing but the list of parts is waited for before they are loaded.
 template <typename T, int D>
 __global__ __launch_bounds__(PA_BLOCK) void paged_join_kernel(PagedAttnArgs a) {
-  const long long id = (long long)blockIdx.x * (PA_BLOCK / 64) + (threadIdx.x >> 6);
+  const unsigned id = blockIdx.x * (PA_BLOCK / 64) + (threadIdx.x >> 6);
   const int lane = threadIdx.x & 63;
-  if (id >= (long long)a.n_rows * a.Hq) return;
-  const int row = (int)(id / a.Hq), head = (int)(id % a.Hq);
-  if (row < a.c.q_off[0] || row >= a.c.q_off[a.c.n_seqs]) return;       // padding
+  if (id >= (unsigned)a.n_rows * (unsigned)a.Hq) return;
+  const int row = (int)(id / (unsigned)a.Hq), head = (int)(id % (unsigned)a.Hq);
   const int2 rp = a.row_parts[id];
-  const long long apart = (long long)a.Hkv * a.block_rows;
-  if (rp.y <= 1 || rp.x < 0 || rp.x + (rp.y - 1) * apart >= a.part_rows) return;
-  constexpr int PIECES = D / 4, GROUPS = 64 / PIECES;                   // groups of lanes take every GROUPS-th part
+  if (row < a.c.q_off[0] || row >= a.c.q_off[a.c.n_seqs]) return;       // padding
+  const long long apart = a.apart;
+  if (rp.y <= 1 || rp.x < 0 || rp.x + (rp.y - 1) * apart - a.shift >= a.part_rows) return;
+  constexpr int PIECES = D / 4, GROUPS = 64 / PIECES, AHEAD = 4;
   const int part = lane % PIECES, grp = lane / PIECES;
-  float M = -INFINITY;
-  for (int k = lane; k < rp.y; k += 64) M = fmaxf(M, a.part_ml[2 * (rp.x + k * apart)]);
+  const floatx4 none = {0.f, 0.f, 0.f, 0.f};
+  floatx4 acc = none;
+  float M = -INFINITY, L = 0.f;
+  for (int k0 = grp; k0 < rp.y; k0 += AHEAD * GROUPS) {
+    float m[AHEAD], l[AHEAD];
+    floatx4 v[AHEAD];
 #pragma unroll
-  for (int d = 1; d < 64; d <<= 1) M = fmaxf(M, __shfl_xor(M, d));
-  floatx4 acc = {0.f, 0.f, 0.f, 0.f};
-  float L = 0.f;
-#pragma unroll 4
-  for (int k = grp; k < rp.y; k += GROUPS) {
-    const long long at = rp.x + k * apart;
-    const float m = a.part_ml[2 * at], l = a.part_ml[2 * at + 1];
-    if (l == 0.f) continue;
-    const float f = m == M ? 1.f : exp2f(m - M);
-    L += l * f;
-    acc += *reinterpret_cast<const floatx4*>(&a.part_o[at * D + 4 * part]) * f;
+    for (int i = 0; i < AHEAD; ++i) {
+      const int k = k0 + i * GROUPS;
+      const int in = k < rp.y ? k : k0;
+      const long long at = rp.x + (in > 0 ? in * apart - a.shift : 0);
+      m[i] = a.part_ml[2 * at];
+      l[i] = k < rp.y ? a.part_ml[2 * at + 1] : 0.f;
+      v[i] = *reinterpret_cast<const floatx4*>(&a.part_o[at * D + 4 * part]);
+    }
+    float to = M;
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i) to = l[i] != 0.f ? fmaxf(to, m[i]) : to;      // (sums of 0: the part had nothing for this row)
+    const float f = to == M ? 1.f : exp2f(M - to);
+    L *= f;
+    acc *= f;
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i) {
+      const float g = m[i] == to ? 1.f : exp2f(m[i] - to);
+      L += l[i] != 0.f ? l[i] * g : 0.f;
+      acc += l[i] != 0.f ? v[i] * g : none;
+    }
+    M = to;
   }
+  float to = M;
+#pragma unroll
+  for (int d = PIECES; d < 64; d <<= 1) to = fmaxf(to, __shfl_xor(to, d));
+  const float f = M == to ? 1.f : exp2f(M - to);
+  L *= f;
+  acc *= f;
 #pragma unroll
   for (int d = PIECES; d < 64; d <<= 1) {
     L += __shfl_xor(L, d);
 #pragma unroll
     for (int i = 0; i < 4; ++i) acc[i] += __shfl_xor(acc[i], d);
   }
-  if (grp == 0) write_row<T, D>(a, row, head, part, M, L, acc);
+  if (grp == 0) write_row<T, D>(a, row, head, part, to, L, acc);
 }
 
 // How a call is cut up.
@@ -815,22 +896,29 @@ Plan plan(const dsbd_paged_kv* c, int n_rows, int Hq, int Hkv, int D, PagedAttnA
   Plan p;
   const long long group = Hq / Hkv, most = (long long)std::min(c->max_new, n_rows) * group;     // rows of a sequence and KV head
   p.rows = most <= 16 ? 16 : most <= 32 ? 32 : most <= 128 ? 128 : 256;
-  const long long slots = p.rows <= 32 ? PA_SLOTS : p.rows == 128 ? PA_TILE_SLOTS : PA_TILE_SLOTS / 2;
-  const long long units = ((long long)n_rows * group / p.rows + c->n_seqs) * Hkv;      // at most
-  p.splits = units < 2 * slots;
-  p.grid = units + (p.splits ? (slots + Hkv - 1) / Hkv * Hkv : 0);
+  const bool wave = p.rows <= 32;
+  const long long slots = wave ? PA_SLOTS : p.rows == 128 ? PA_TILE_SLOTS : PA_TILE_SLOTS / 2;
+  // Few units: what is split may be joined, in a workspace that depends on the shapes alone.  Sequences of up to 256 tokens
+  // stay whole all the same: one token for each of 2 sequences of 255 tokens, 32 heads, 10.2 us against 11.9; of 511, 14.0 against 11.9.
+  const long long units = wave ? (long long)c->n_seqs * Hkv : ((long long)n_rows * group / p.rows + c->n_seqs) * Hkv;      // at most
+  const bool few = units < 2 * slots;
+  const int per_head = (int)std::max<long long>(slots / Hkv, 1);
+  p.splits = few && c->max_len > 256;
+  const long long parts = wave ? 2ll * per_head * Hkv : units + (slots + Hkv - 1) / Hkv * Hkv;
+  p.grid = wave ? p.splits ? (long long)per_head * Hkv : units : p.splits ? parts : units;
   WorkspaceCarver w(workspace);
   float *po = nullptr, *ml = nullptr;
   int2* rp = nullptr;
-  if (p.splits) {
+  if (few) {
     rp = w.take<int2>((size_t)n_rows * Hq);
-    ml = w.take<float>((size_t)p.grid * p.rows * 2);
-    po = w.take<float>((size_t)p.grid * p.rows * D);
+    ml = w.take<float>((size_t)parts * p.rows * 2);
+    po = w.take<float>((size_t)parts * p.rows * D);
   }
   p.bytes = std::max<size_t>(w.total(), 256);
   if (a) {
     a->splits = p.splits; a->part_o = po; a->part_ml = ml; a->row_parts = rp;
-    a->part_rows = p.grid * p.rows; a->block_rows = p.rows;
+    a->part_rows = parts * p.rows; a->block_rows = p.rows; a->per_head = per_head;
+    a->apart = (wave ? 2 : 1) * (long long)Hkv * p.rows; a->shift = wave ? (long long)Hkv * p.rows : 0;
   }
   return p;
 }
@@ -868,7 +956,7 @@ extern "C" int32_t dsbd_paged_attention(const dsbd_paged_kv* cache, int32_t n_ro
   PagedAttnArgs a;
   const Plan p = plan(cache, n_rows, Hq, Hkv, D, &a, workspace);
   if (workspace_bytes < p.bytes) return DSBD_ERR_WORKSPACE;
-  if (p.grid > 0x7fffffffLL / p.rows) return DSBD_ERR_UNSUPPORTED;
+  if (a.part_rows > 0x7fffffffLL || p.grid > 0x7fffffffLL) return DSBD_ERR_UNSUPPORTED;
   a.c = paged_args(cache);
   a.k_pages = cache->k_pages; a.v_pages = cache->v_pages; a.q = q->ptr; a.out = out->ptr; a.lse = lse; a.anc = anc_mask;
   a.q_tok = q->token_stride; a.q_head = q->head_stride; a.o_tok = out->token_stride; a.o_head = out->head_stride;
