@@ -1,13 +1,17 @@
 // Attention of a chunk of new tokens over a paged cache (dsbd_paged_attention).
 //
 // The rows of a KV head of one sequence are its new tokens times the query heads of the group, token-major: row r is token
-// r / group, head r % group, so whatever shares keys shares a workgroup.  A unit is (sequence, block of rows, KV head); the
-// keys that a unit sees are cut into parts where there are fewer units than the device takes at once, and the parts' results
-// (unnormalised output, reference exponent, sum) are joined by a second kernel.
+// r / group, head r % group, so whatever shares keys shares a workgroup.  Up to 32 rows: the wave-private kernel, which streams the
+// caches; above, the tile kernel, which is bound by its matrix products and exponentials.  Either cuts the keys into parts where
+// there are fewer rows than the device takes at once; the parts' results (unnormalised output, reference exponent, sum) are joined
+// by a second kernel.
 //
-// Wave-private kernel: each of the 4 waves takes 32-token steps of its own from memory through registers into its LDS tiles;
+// Wave-private kernel: each of the 4 waves takes 32-token steps of its own from memory through registers, a step ahead, into its
+// LDS tiles;
 //   S^T = K Q^T    MFMA 16x16x32, Q^T held in registers: a lane owns one query row, so the softmax stays inside the lane;
 //   O^T += V^T P^T MFMA 16x16x32, P^T from the registers of S^T, V^T by the transposing LDS read.
+// 8 heads of 128, bf16: one token for each of 64 sequences of 8192 tokens 342 us (6.3 TB/s of K and V; a plain streaming read makes
+// 7.0); of 32 sequences of 1024 to 8192 tokens 111 us (5.8 TB/s); two of 32 tokens, 4 heads of 64, 6 us.
 #include "common.h"
 #include "paged.h"
 #include "wave_f64.h"
@@ -219,10 +223,16 @@ __device__ __forceinline__ void write_part(const PagedAttnArgs& a, long long slo
 // Workgroup barrier that orders LDS traffic only (loads in flight stay in flight).
 __device__ __forceinline__ void lds_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 
+// One lane's value.
+__device__ __forceinline__ long long lane_value(long long v, int l) {
+  const unsigned lo = __builtin_amdgcn_readlane((int)(unsigned)v, l), hi = __builtin_amdgcn_readlane((int)(v >> 32), l);
+  return (long long)((unsigned long long)hi << 32 | lo);
+}
+
 // Whatever a workgroup has to do: where there are too few (sequence, KV head) to fill the device, the steps of all sequences, one
 // behind the other, are cut into `per_head` even ranges, a workgroup each and KV head.  So all workgroups end together whatever the
 // lengths are; a range may end one sequence, take others whole and begin another, and has room for two partial results.  (One token for
-// each of 32 sequences of 1024 to 8192 tokens: even parts of each sequence 122 us, ranges @RANGES us.)  The sequences' lengths lie in
+// each of 32 sequences of 1024 to 8192 tokens: even parts of each sequence 122 us, ranges 111.)  The sequences' lengths lie in
 // device memory, so every wave looks for its place itself, a lane per sequence, 64 at a time.
 template <typename T, int D, int NRT>
 __global__ __launch_bounds__(PA_BLOCK, 2) void paged_wave_kernel(PagedAttnArgs a) {
@@ -238,31 +248,31 @@ __global__ __launch_bounds__(PA_BLOCK, 2) void paged_wave_kernel(PagedAttnArgs a
   __shared__ unsigned lost[ROWS][D / 16];
   __shared__ int any_lost;
 
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = lane & 15, qd = lane >> 4;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 15, qd = lane >> 4;
   const int b = quotient(a.heads, blockIdx.x), g = blockIdx.x - b * a.Hkv;      // (workgroups go to the 8 dies in turn)
   // ---- this workgroup's range, and the sequence that it begins in
   int s0 = 0, steps = 0;                       // the first of the 64 sequences at hand; steps of this lane's
-  long long begin = 0, upto = 0;               // where they begin, and where the last of the 64 ends
-  auto scan = [&](int from, long long base) {
-    s0 = from; steps = 0;
+  long long begin = 0, base = 0, next = 0;     // where they begin; where the first does, and the one behind the last
+  auto scan = [&](int from, long long at) {
+    s0 = from; steps = 0; base = at;
     if (s0 + lane < a.c.n_seqs) {
       const Seq q = sequence(a, s0 + lane);
       if (q.torn) atomicOr(a.fault, DSBD_FAULT_BOUNDS);
       steps = q.n == 0 ? 0 : q.good ? (q.ctx + q.n + PA_STEP - 1) / PA_STEP : 1;
     }
-    upto = steps;
+    long long upto = steps;
 #pragma unroll
     for (int d = 1; d < 64; d <<= 1) { const long long o = __shfl_up(upto, d); if (lane >= d) upto += o; }
     begin = base + upto - steps;
-    upto = base + __shfl(upto, 63);
+    next = base + lane_value(upto, 63);
   };
   long long x = 0, x_end = 0, per = 0;
   if (a.splits) {
     scan(0, 0);
-    while (s0 + 64 < a.c.n_seqs) scan(s0 + 64, upto);
-    per = max((long long)ceil((double)upto / a.per_head), (long long)PA_MIN_STEPS);
+    while (s0 + 64 < a.c.n_seqs) scan(s0 + 64, next);
+    per = lane_value(max((long long)ceil((double)next / a.per_head), (long long)PA_MIN_STEPS), 0);
     x = b * per;
-    x_end = min(x + per, upto);
+    x_end = min(x + per, next);
     if (x >= x_end) return;
     if (s0 > 0) scan(0, 0);
   }
@@ -272,12 +282,12 @@ __global__ __launch_bounds__(PA_BLOCK, 2) void paged_wave_kernel(PagedAttnArgs a
       unsigned long long m = __ballot(x >= begin && x < begin + steps);
       while (!m) {
         if (s0 + 64 >= a.c.n_seqs) return;
-        scan(s0 + 64, upto);
+        scan(s0 + 64, next);
         m = __ballot(x >= begin && x < begin + steps);
       }
       const int l = (int)__ffsll((long long)m) - 1;
       s = s0 + l;
-      const long long first = __shfl(begin, l);
+      const long long first = lane_value(begin, l);
       const int n = __builtin_amdgcn_readlane(steps, l);
       st_begin = (int)(x - first);
       st_end = (int)min(x_end - first, (long long)n);
@@ -288,7 +298,7 @@ __global__ __launch_bounds__(PA_BLOCK, 2) void paged_wave_kernel(PagedAttnArgs a
     const Seq sq = sequence(a, s);
     const int R = sq.n * a.group.d, len = sq.ctx + sq.n;
     if (g == 0 && st_begin == 0 && threadIdx.x == 0 && (sq.torn || (sq.n > 0 && !sq.good))) atomicOr(a.fault, DSBD_FAULT_BOUNDS);
-    if (R == 0) continue;
+    if (R == 0) return;                        // (no range has it)
     if (!sq.good) {                            // (any number of rows)
       for (long long i = threadIdx.x; i < (long long)R * (D / 4); i += PA_BLOCK) {
         const int r = (int)(i / (D / 4)), part = (int)(i % (D / 4)), tok = quotient(a.group, r), head = g * a.group.d + r - tok * a.group.d;
@@ -504,6 +514,7 @@ __global__ __launch_bounds__(PA_BLOCK, 2) void paged_wave_kernel(PagedAttnArgs a
       if (a.splits && part == 0 && st_begin == 0) a.row_parts[row * a.Hq + head] = make_int2((int)slot + r, nparts);
     }
     __syncthreads();                             // (the LDS, for the next)
+    if (a.splits && x < x_end) scan(s0, base);     // (again: the registers have had other use)
   } while (a.splits && x < x_end);
 }
 
@@ -895,6 +906,8 @@ struct Plan {
 Plan plan(const dsbd_paged_kv* c, int n_rows, int Hq, int Hkv, int D, PagedAttnArgs* a, void* workspace) {
   Plan p;
   const long long group = Hq / Hkv, most = (long long)std::min(c->max_new, n_rows) * group;     // rows of a sequence and KV head
+  // (17 to 32 rows, in the wave-private kernel and in the tile kernel: 7 nodes for each of 32 sequences of 1024 to 8192 tokens, 4 heads per
+  // KV head, 141 us against 156; for each of 8 sequences of 8000 tokens 73 us against 66)
   p.rows = most <= 16 ? 16 : most <= 32 ? 32 : most <= 128 ? 128 : 256;
   const bool wave = p.rows <= 32;
   const long long slots = wave ? PA_SLOTS : p.rows == 128 ? PA_TILE_SLOTS : PA_TILE_SLOTS / 2;
