@@ -267,3 +267,32 @@ def test_two_streams_at_once_and_two_graphs_of_one_pool():
             a, b = outs[i][0].clone(), outs[i][1].clone()
             want = dsbd.dsbd_paged_attention(cache, q)
             assert torch.equal(a, want[0]) and torch.equal(b, want[1])
+
+
+@pytest.mark.parametrize("lens,Hq,Hk", [([(260 + 7 * (i % 11), 1) for i in range(150)], 16, 8), ([(400, 1), (90, 1)], 80, 40),
+                                        ([(0, 0)] + [(300 + i, 9 + i % 5) for i in range(72)], 32, 8), ([(2, 140), (900, 130)], 24, 24)],
+                         ids=["more sequences than are cut", "40 heads", "many trees", "many heads of a chunk"])
+def test_many_units(lens, Hq, Hk):
+    """Calls with enough (sequence, KV head) to fill the device, which split nothing, and head numbers that divide it unevenly."""
+    import paper_2409_16560_amd as dsbd
+    gen = torch.Generator().manual_seed(38)
+    cache, table, off, N = make_cache(gen, lens, 16, Hk, 64, BF16)
+    q = randn(gen, N, Hq, 64)
+    out, lse, fault = dsbd.dsbd_paged_attention(cache, q)
+    assert int(fault) == 0
+    check(cache, table, off, lens, q, out, lse, rows=3)
+
+
+@pytest.mark.parametrize("n", [1, 12, 90])
+def test_tokens_behind_the_tables_end(n):
+    """A table that ends inside a sequence: its further tokens count as not there, and are reported."""
+    import paper_2409_16560_amd as dsbd
+    gen = torch.Generator().manual_seed(39)
+    lens = [(500, n), (100, n)]
+    cache, table, off, N = make_cache(gen, lens, 16, 2, 128, F16)
+    table = np.ascontiguousarray(table[:, :14])
+    cache.page_table = torch.from_numpy(table).cuda()
+    q = randn(gen, N, 4, 128, dtype=F16)
+    out, lse, fault = dsbd.dsbd_paged_attention(cache, q)
+    assert int(fault) == dsbd.DSBD_FAULT_BOUNDS
+    check(cache, table, off, lens, q, out, lse, rows=8)
