@@ -7,7 +7,8 @@
 // first; what a row's path adds is then the population count of (its ancestors & the nodes with that token).  Every thread keeps
 // the places of its 16 tokens that have a word or a bias as a bit per piece and streams row after row, without a barrier between rows of a tree, the
 // next row's loads on their way during a row's arithmetic.
-// Bound by HBM: logits are read once and written once, a piece that a mask excludes as a whole is not read at all.
+// Bound by HBM: logits are read once and written once, a piece that a mask excludes as a whole is not read at all: 191 rows of 128256
+// f32 with every rule 46.5 us, 198 MB at 4.3 TB/s (a large copy makes 5.2).  By latency where there are few rows: 7 us.
 #include "common.h"
 #include "paged.h"
 #include "topology_device.h"
