@@ -23,6 +23,7 @@ namespace {
 #define PA_STEP 32                 // tokens per wave step
 #define PA_SLOTS 512               // workgroups of the wave-private kernel that the device holds (70 KB of LDS each)
 #define PA_MIN_STEPS 4             // steps that a part has at least
+#define PA_TILE 64                 // tokens per tile
 #define PA_TILE_SLOTS 512          // workgroups of 4 waves of the tile kernel that the device holds; half as many of 8
 
 typedef float floatx4 __attribute__((ext_vector_type(4)));
@@ -70,6 +71,7 @@ struct PagedAttnArgs {
   long long part_rows;                         // rows of part_o
   int block_rows;
   long long apart, shift;                      // row of part k > 0 of a row: the first one's + k * apart - shift
+  int join;                                    // (row, head) per wave of the join kernel
   int per_head;                                // ranges of the wave-private kernel
   int32_t* fault;
 };
@@ -89,47 +91,98 @@ __device__ __forceinline__ Seq sequence(const PagedAttnArgs& a, int s) {
 
 struct Unit { int s, g, rb, part, nparts; };
 
-// Which unit, and which part of it, a workgroup has: lengths lie in device memory, so every wave works it out for itself, a
-// lane per sequence (64 at a time).  A unit is cut into even parts of at most `len` steps, where len is the shortest, to within a
-// sixteenth, that makes no more parts than the device holds workgroups, so that all run at once and end together; units that
-// are more than half as many as that are cut at an even share of all steps.  False: nothing to do.
-template <int STEP>
-__device__ __forceinline__ bool find_unit(const PagedAttnArgs& a, int slots, Unit& u, int& part_steps) {
+// Which unit (sequence, block of rows, KV head) a workgroup of the tile kernel has, and which part of it: lengths lie in device
+// memory, so every wave works it out for itself, a lane per sequence, 64 at a time.
+//   Units that the device does not hold at once: longest first, so that they end together; what is a quarter longer than an even share is cut.
+//   (Three chunks of 600 to 2100 tokens behind up to 4100, 432 units for 256 workgroups: sequence by sequence, cut at the even share,
+//   228 us, longest first 211, cut a quarter later 195.)
+//   Fewer: even parts of at most `len` steps, where len is the shortest, to within a sixteenth, that makes no more parts than the
+//   device holds workgroups.
+// False: nothing to do.
+__device__ __forceinline__ bool find_unit(const PagedAttnArgs& a, int slots, Unit& u, int& part_tiles) {
   const int lane = threadIdx.x & 63, rows = a.block_rows;
   // The head changes fastest: workgroups go to the 8 dies in turn, so that with 8 heads or a multiple what a die has in hand shares
   // the keys in its L2.
   const int at = quotient(a.heads, blockIdx.x);
   u.g = blockIdx.x - at * a.Hkv;
-  int nrb, steps, have = -1;
+  Seq q;
+  int nrb, longest, have = -1;                 // this lane's sequence: blocks of rows, tiles that its last block sees
   auto measure = [&](int s0) {
     if (s0 == have) return;
-    have = s0; nrb = 0; steps = 0;
+    have = s0; nrb = 0; longest = 0;
     if (s0 + lane < a.c.n_seqs) {
-      const Seq q = sequence(a, s0 + lane);
+      q = sequence(a, s0 + lane);
       if (q.torn) atomicOr(a.fault, DSBD_FAULT_BOUNDS);
       nrb = (int)(((long long)q.n * a.group.d + rows - 1) / rows);
-      steps = q.good ? (q.ctx + q.n + STEP - 1) / STEP : 1;
+      longest = q.good ? (q.ctx + q.n + PA_TILE - 1) / PA_TILE : 1;
     }
   };
-  auto count = [&](int len) { return steps > len ? (int)((unsigned)(steps + len - 1) / (unsigned)len) : 1; };
-  int len = 0x7fffffff;
-  if (a.splits) {
-    double total = 0.0, units = 0.0;
+  const bool several = a.c.n_seqs > 1 && a.c.n_seqs <= 64;      // (the blocks of one sequence are in order as they are)
+  double seen = 0.0, full = 0.0, units = 0.0;  // tiles that the blocks see, about; as if all saw the last one's
+  if (a.splits || several) {
     for (int s0 = 0; s0 < a.c.n_seqs; s0 += 64) {
       measure(s0);
-      total += (double)nrb * (double)steps;
+      const int first = !q.good || a.anc ? longest : (q.ctx + min(quotient(a.group, rows), q.n) + PA_TILE - 1) / PA_TILE;
+      seen += 0.5 * (double)nrb * ((double)first + (double)longest);
+      full += (double)nrb * (double)longest;
       units += (double)nrb;
     }
-    total = wave_sum(total) * a.Hkv;
     units = wave_sum(units) * a.Hkv;
-    len = max((int)fmin(ceil(total / slots), 1e9), PA_MIN_STEPS);
+  }
+  if (several && units > slots) {
+    int cut = a.splits ? max((int)fmin(ceil(1.25 * wave_sum(seen) * a.Hkv / slots), 1e9), PA_MIN_STEPS) : 0x7fffffff;
+    // blocks of this lane's sequence that see at least t tiles (the last ones), and the parts that they make
+    auto blocks = [&](int t) {
+      if (nrb == 0 || t > longest) return 0;
+      const long long x = !q.good || a.anc ? 0ll : 64ll * (t - 1) - q.ctx;      // a block sees t tiles if its last token is x or a later one
+      return x <= 0 ? nrb : nrb - ((int)(x * a.group.d) >> (__ffs(rows) - 1));      // (rows: a power of two; no more of them than int holds)
+    };
+    auto parts = [&](int t) {
+      int n = blocks(t);
+      for (long long more = (long long)cut + 1; more <= longest; more += cut) n += blocks((int)max((long long)t, more));
+      return n;
+    };
+    while (cut < (1 << 29) && wave_sum((double)parts(1)) * a.Hkv > (double)gridDim.x) cut *= 2;
+    auto upto = [&](int n) {                   // inclusive sum over the lanes
+#pragma unroll
+      for (int d = 1; d < 64; d <<= 1) { const int o = __shfl_up(n, d); if (lane >= d) n += o; }
+      return n;
+    };
+    // the number of tiles t that the unit sees: more than `at` parts have t or more, at most `at` more than t
+    int lo = 0, hi = longest + 1;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) hi = max(hi, __shfl_xor(hi, d));
+    hi = __builtin_amdgcn_readfirstlane(hi);     // (the same in all lanes: what depends on it stays in scalar registers)
+    cut = __builtin_amdgcn_readfirstlane(cut);
+    while (hi - lo > 1) {
+      const int mid = lo + (hi - lo) / 2;
+      if (wave_sum((double)parts(mid)) > (double)at) lo = mid; else hi = mid;
+    }
+    if (lo == 0) return false;
+    const int behind = parts(lo + 1), mine = parts(lo) - behind;
+    const int incl = upto(mine), rank = at - (int)wave_sum((double)behind);
+    const unsigned long long m = __ballot(rank >= incl - mine && rank < incl);
+    if (!m) return false;
+    const int l = (int)__ffsll((long long)m) - 1;
+    u.s = l;
+    u.nparts = (int)((unsigned)(lo - 1) / (unsigned)cut) + 1;
+    part_tiles = (int)((unsigned)(lo + u.nparts - 1) / (unsigned)u.nparts);
+    const int rel = rank - __builtin_amdgcn_readlane(incl - mine, l), block = rel / u.nparts;
+    u.part = rel - block * u.nparts;
+    u.rb = __builtin_amdgcn_readlane(nrb - blocks(lo + 1), l) - 1 - block;
+    return u.rb >= 0;
+  }
+  auto count = [&](int len) { return longest > len ? (int)((unsigned)(longest + len - 1) / (unsigned)len) : 1; };
+  int len = 0x7fffffff;
+  if (a.splits) {
+    len = max((int)fmin(ceil(wave_sum(full) * a.Hkv / slots), 1e9), PA_MIN_STEPS);
     if (2.0 * units <= slots) {
       int hi = 2 * len;                        // enough: at most slots / 2 parts of that length, and one more for each unit
       while (hi - len > max(len / 16, 1)) {    // (at least 2 apart: mid lies between them)
         const int mid = (len + hi) / 2;
-        double parts = 0.0;
-        for (int s0 = 0; s0 < a.c.n_seqs; s0 += 64) { measure(s0); parts += (double)nrb * count(mid); }
-        if (wave_sum(parts) * a.Hkv <= slots) hi = mid; else len = mid;
+        double n = 0.0;
+        for (int s0 = 0; s0 < a.c.n_seqs; s0 += 64) { measure(s0); n += (double)nrb * count(mid); }
+        if (wave_sum(n) * a.Hkv <= slots) hi = mid; else len = mid;
       }
       len = hi;
     }
@@ -148,7 +201,7 @@ __device__ __forceinline__ bool find_unit(const PagedAttnArgs& a, int slots, Uni
       const int l = (int)__ffsll((long long)m) - 1;
       u.s = s0 + l;
       u.nparts = __builtin_amdgcn_readlane(np, l);
-      part_steps = (int)((unsigned)(__builtin_amdgcn_readlane(steps, l) + u.nparts - 1) / (unsigned)u.nparts);
+      part_tiles = (int)((unsigned)(__builtin_amdgcn_readlane(longest, l) + u.nparts - 1) / (unsigned)u.nparts);
       const int rel = at - (int)__builtin_amdgcn_readlane((int)begin, l);
       const int n = __builtin_amdgcn_readlane(nrb, l), block = rel / u.nparts;
       u.part = rel - block * u.nparts;
@@ -524,14 +577,13 @@ __global__ __launch_bounds__(PA_BLOCK, 2) void paged_wave_kernel(PagedAttnArgs a
 // in between) a tile ahead; the pieces of a row are swizzled by the token, so that the operand reads, which go down the rows,
 // spread over the banks.  MFMA 32x32x16: S^T = K Q^T and O^T += V^T P^T as in the wave-private kernel, a lane owns a query row
 // together with the lane 32 further on, which has the other half of its tokens.
-#define PA_TILE 64
 
 typedef __attribute__((address_space(3))) void lds_void;
 typedef const __attribute__((address_space(1))) void glb_cvoid;
 
 // NW: waves, 4 where 128 rows hold all of a sequence's (two workgroups per CU), 8 above (one, which fills a tile for twice the rows):
 // 8 trees of 31 nodes with 4 heads per KV head on 8192 tokens 71 us against 88; a prompt of 8192 tokens, 32 heads of 128, 638 us
-// against 582; three chunks of 600 to 2100 tokens 247 us against 234.  RUNS: pages are whole multiples of 8 tokens.
+// against 582; three chunks of 600 to 2100 tokens 247 us against 234 (as they were ordered then).  RUNS: pages are whole multiples of 8 tokens.
 template <typename T, int D, int NW, bool RUNS>
 __global__ __launch_bounds__(64 * NW, 2) void paged_tile_kernel(PagedAttnArgs a) {
   typedef typename Elem<T>::x8 x8;
@@ -546,7 +598,7 @@ __global__ __launch_bounds__(64 * NW, 2) void paged_tile_kernel(PagedAttnArgs a)
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 31, h = lane >> 5;
   Unit u;
   int part_tiles;
-  if (!find_unit<PA_TILE>(a, PA_TILE_SLOTS * 4 / NW, u, part_tiles)) return;
+  if (!find_unit(a, PA_TILE_SLOTS * 4 / NW, u, part_tiles)) return;
   const Seq sq = sequence(a, u.s);
   const int R = sq.n * a.group.d, row0 = u.rb * ROWS, len = sq.ctx + sq.n;
   if (u.g == 0 && u.rb == 0 && u.part == 0 && threadIdx.x == 0 && !sq.good) atomicOr(a.fault, DSBD_FAULT_BOUNDS);
@@ -838,62 +890,72 @@ __global__ __launch_bounds__(64 * NW, 2) void paged_tile_kernel(PagedAttnArgs a)
   }
 }
 
-// A wave per (row, head) of what was split.  Groups of lanes take every GROUPS-th part, four
-// at a time, and carry a maximum and a sum of their own, so that nothing but the list of parts is waited for before they are loaded.
+// A wave takes `join` (row, head) and joins those that were split: one, or, where there are so many that most were not, up to 4, which
+// are looked up together (107808 of them, none split: one each 10.6 us, four 4.5; 7936, all of 8 parts: one each 8.3 us).  Groups of
+// lanes take every GROUPS-th part, four at a time, and carry a maximum and a sum of their own, so that nothing but the list of parts
+// is waited for before they are loaded.
 template <typename T, int D>
 __global__ __launch_bounds__(PA_BLOCK) void paged_join_kernel(PagedAttnArgs a) {
-  const unsigned id = blockIdx.x * (PA_BLOCK / 64) + (threadIdx.x >> 6);
+  const unsigned n = (unsigned)a.n_rows * (unsigned)a.Hq, base = (blockIdx.x * (PA_BLOCK / 64) + (threadIdx.x >> 6)) * (unsigned)a.join;
   const int lane = threadIdx.x & 63;
-  if (id >= (unsigned)a.n_rows * (unsigned)a.Hq) return;
-  const int row = (int)(id / (unsigned)a.Hq), head = (int)(id % (unsigned)a.Hq);
-  const int2 rp = a.row_parts[id];
-  if (row < a.c.q_off[0] || row >= a.c.q_off[a.c.n_seqs]) return;       // padding
-  const long long apart = a.apart;
-  if (rp.y <= 1 || rp.x < 0 || rp.x + (rp.y - 1) * apart - a.shift >= a.part_rows) return;
+  if (base >= n) return;
+  int2 mine = make_int2(0, 0);                 // this lane's (row, head): its first part and their number
+  bool split = false;
+  if (lane < a.join && base + lane < n) {
+    mine = a.row_parts[base + lane];
+    const int row = (int)((base + lane) / (unsigned)a.Hq);
+    split = row >= a.c.q_off[0] && row < a.c.q_off[a.c.n_seqs] &&       // (not padding)
+            mine.y > 1 && mine.x >= 0 && mine.x + (mine.y - 1) * a.apart - a.shift < a.part_rows;
+  }
   constexpr int PIECES = D / 4, GROUPS = 64 / PIECES, AHEAD = 4;
   const int part = lane % PIECES, grp = lane / PIECES;
   const floatx4 none = {0.f, 0.f, 0.f, 0.f};
-  floatx4 acc = none;
-  float M = -INFINITY, L = 0.f;
-  for (int k0 = grp; k0 < rp.y; k0 += AHEAD * GROUPS) {
-    float m[AHEAD], l[AHEAD];
-    floatx4 v[AHEAD];
+  for (unsigned long long m = __ballot(split); m; m &= m - 1) {
+    const int who = (int)__ffsll((long long)m) - 1;
+    const int2 rp = make_int2(__builtin_amdgcn_readlane(mine.x, who), __builtin_amdgcn_readlane(mine.y, who));
+    const int row = (int)((base + who) / (unsigned)a.Hq), head = (int)((base + who) % (unsigned)a.Hq);
+    floatx4 acc = none;
+    float M = -INFINITY, L = 0.f;
+    for (int k0 = grp; k0 < rp.y; k0 += AHEAD * GROUPS) {
+      float x[AHEAD], l[AHEAD];
+      floatx4 v[AHEAD];
 #pragma unroll
-    for (int i = 0; i < AHEAD; ++i) {
-      const int k = k0 + i * GROUPS;
-      const int in = k < rp.y ? k : k0;
-      const long long at = rp.x + (in > 0 ? in * apart - a.shift : 0);
-      m[i] = a.part_ml[2 * at];
-      l[i] = k < rp.y ? a.part_ml[2 * at + 1] : 0.f;
-      v[i] = *reinterpret_cast<const floatx4*>(&a.part_o[at * D + 4 * part]);
+      for (int i = 0; i < AHEAD; ++i) {
+        const int k = k0 + i * GROUPS;
+        const int in = k < rp.y ? k : k0;
+        const long long at = rp.x + (in > 0 ? in * a.apart - a.shift : 0);
+        x[i] = a.part_ml[2 * at];
+        l[i] = k < rp.y ? a.part_ml[2 * at + 1] : 0.f;
+        v[i] = *reinterpret_cast<const floatx4*>(&a.part_o[at * D + 4 * part]);
+      }
+      float to = M;
+#pragma unroll
+      for (int i = 0; i < AHEAD; ++i) to = l[i] != 0.f ? fmaxf(to, x[i]) : to;      // (sums of 0: the part had nothing for this row)
+      const float f = to == M ? 1.f : exp2f(M - to);
+      L *= f;
+      acc *= f;
+#pragma unroll
+      for (int i = 0; i < AHEAD; ++i) {
+        const float g = x[i] == to ? 1.f : exp2f(x[i] - to);
+        L += l[i] != 0.f ? l[i] * g : 0.f;
+        acc += l[i] != 0.f ? v[i] * g : none;
+      }
+      M = to;
     }
     float to = M;
 #pragma unroll
-    for (int i = 0; i < AHEAD; ++i) to = l[i] != 0.f ? fmaxf(to, m[i]) : to;      // (sums of 0: the part had nothing for this row)
-    const float f = to == M ? 1.f : exp2f(M - to);
+    for (int d = PIECES; d < 64; d <<= 1) to = fmaxf(to, __shfl_xor(to, d));
+    const float f = M == to ? 1.f : exp2f(M - to);
     L *= f;
     acc *= f;
 #pragma unroll
-    for (int i = 0; i < AHEAD; ++i) {
-      const float g = m[i] == to ? 1.f : exp2f(m[i] - to);
-      L += l[i] != 0.f ? l[i] * g : 0.f;
-      acc += l[i] != 0.f ? v[i] * g : none;
+    for (int d = PIECES; d < 64; d <<= 1) {
+      L += __shfl_xor(L, d);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) acc[i] += __shfl_xor(acc[i], d);
     }
-    M = to;
+    if (grp == 0) write_row<T, D>(a, row, head, part, to, L, acc);
   }
-  float to = M;
-#pragma unroll
-  for (int d = PIECES; d < 64; d <<= 1) to = fmaxf(to, __shfl_xor(to, d));
-  const float f = M == to ? 1.f : exp2f(M - to);
-  L *= f;
-  acc *= f;
-#pragma unroll
-  for (int d = PIECES; d < 64; d <<= 1) {
-    L += __shfl_xor(L, d);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) acc[i] += __shfl_xor(acc[i], d);
-  }
-  if (grp == 0) write_row<T, D>(a, row, head, part, to, L, acc);
 }
 
 // How a call is cut up.
@@ -980,7 +1042,8 @@ extern "C" int32_t dsbd_paged_attention(const dsbd_paged_kv* cache, int32_t n_ro
   a.fault = fault;
   hipStream_t stream = static_cast<hipStream_t>(stream_);
   const dim3 grid((unsigned)p.grid), block(PA_BLOCK);
-  const dim3 join((unsigned)(((long long)n_rows * Hq + PA_BLOCK / 64 - 1) / (PA_BLOCK / 64)));
+  a.join = (int)std::min(4ll, 1 + (long long)n_rows * Hq / 16384);
+  const dim3 join((unsigned)(((long long)n_rows * Hq + a.join * (PA_BLOCK / 64) - 1) / (a.join * (PA_BLOCK / 64))));
 #define PA_TILES(T, DD, NW)                                                                                \
   do {                                                                                                     \
     if (a.page_run == 8) hipLaunchKernelGGL((paged_tile_kernel<T, DD, NW, true>), grid, dim3(64 * NW), 0, stream, a); \
