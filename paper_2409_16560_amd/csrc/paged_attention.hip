@@ -22,7 +22,7 @@ namespace {
 #define PA_BLOCK 256
 #define PA_STEP 32                 // tokens per wave step
 #define PA_SLOTS 512               // workgroups of the wave-private kernel that the device holds (70 KB of LDS each)
-#define PA_MIN_STEPS 4             // steps that a part has at least
+#define PA_MIN_STEPS 4             // steps that a part has at least (one token behind each of 2 x 511, 32 heads: 11.9 us; with 8 14.0)
 #define PA_TILE 64                 // tokens per tile
 #define PA_TILE_SLOTS 512          // workgroups of 4 waves of the tile kernel that the device holds; half as many of 8
 
@@ -93,7 +93,8 @@ struct Unit { int s, g, rb, part, nparts; };
 
 // Which unit (sequence, block of rows, KV head) a workgroup of the tile kernel has, and which part of it: lengths lie in device
 // memory, so every wave works it out for itself, a lane per sequence, 64 at a time.
-//   Units that the device does not hold at once: longest first, so that they end together; what is a quarter longer than an even share is cut.
+//   Units that the device does not hold at once: longest first, so that they end together; what is a quarter longer than an even
+//   share is cut.
 //   (Three chunks of 600 to 2100 tokens behind up to 4100, 432 units for 256 workgroups: sequence by sequence, cut at the even share,
 //   228 us, longest first 211, cut a quarter later 195.)
 //   Fewer: even parts of at most `len` steps, where len is the shortest, to within a sixteenth, that makes no more parts than the
@@ -583,7 +584,9 @@ typedef const __attribute__((address_space(1))) void glb_cvoid;
 
 // NW: waves, 4 where 128 rows hold all of a sequence's (two workgroups per CU), 8 above (one, which fills a tile for twice the rows):
 // 8 trees of 31 nodes with 4 heads per KV head on 8192 tokens 71 us against 88; a prompt of 8192 tokens, 32 heads of 128, 638 us
-// against 582; three chunks of 600 to 2100 tokens 247 us against 234 (as they were ordered then).  RUNS: pages are whole multiples of 8 tokens.
+// against 582; three chunks of 600 to 2100 tokens 247 us against 234 (as they were ordered then).  RUNS: pages are whole multiples of
+// 8 tokens, so what a load instruction takes begins at one address and needs no place of its own in every lane (the prompt 616 us
+// against 655, in the form of 4 waves).
 template <typename T, int D, int NW, bool RUNS>
 __global__ __launch_bounds__(64 * NW, 2) void paged_tile_kernel(PagedAttnArgs a) {
   typedef typename Elem<T>::x8 x8;
