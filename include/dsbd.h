@@ -472,7 +472,8 @@ int32_t dsbd_paged_append(const dsbd_paged_kv* cache, int32_t n_rows, int32_t Hq
  *   q     [n_rows,Hq,D] DSBD_BF16 or DSBD_F16, the pages' type; out the same; lse [n_rows,Hq] f32 natural logarithm, or NULL
  *   scale <= 0 selects 1/sqrt(D)
  * A row that sees nothing gets 0 and a lse of -Inf.  Slots behind a sequence's last token are never used, whatever they
- * hold, and neither is what a row does not see, NaN and Inf among it.
+ * hold, and neither is what a row does not see, NaN and Inf among it.  NaN in a row's query or in a key that it sees, and a
+ * score of +Inf, make the row and its lse NaN; a score of -Inf has no weight.
  * Sequences with lengths outside the bounds raise DSBD_FAULT_BOUNDS and get rows of 0 and -Inf; so do, for the tokens of
  * that page alone (they count as not there), page indices outside [0, n_pages).
  * Supported: D = 128 or 64, Hq % Hkv == 0.

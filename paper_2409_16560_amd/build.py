@@ -12,13 +12,12 @@ SOURCES = ["attention.hip", "verify.hip", "verify_rows.hip", "select.hip", "comm
            "qk_rows.hip", "paged_attention.hip", "logits.hip"]
 # Per-file flags.  attention.hip: scores come out of the matrix units and go through max / exp2 only; without
 # -fno-honor-nans every fmaxf operand is first canonicalised (v_max x, x), which triples the instructions of the
-# row-maximum checks; paged_attention.hip likewise.  (verify.hip must keep NaN semantics: it detects non-finite logits.)
+# row-maximum checks.  (verify.hip must keep NaN semantics: it detects non-finite logits.)
 # verify.hip: the layer kernel is held to 240 registers (an attribute in the source; 215 plain, 127 warped, 172 where
 # warped records are sums alone); hoisting loop-invariant address arithmetic out of its layer loop (machine LICM) made it spill 84-120 bytes per
 # lane, with reloads in front of stores on the critical path.
 # (-Rpass-analysis: the compiler's per-kernel register report, checked below)
 FILE_FLAGS = {"attention.hip": os.environ.get("DSBD_ATTN_FLAGS", "-fno-honor-nans").split(),
-              "paged_attention.hip": ["-fno-honor-nans"],
               "verify.hip": os.environ.get("DSBD_VERIFY_FLAGS", "-mllvm -disable-machine-licm").split()
               + ["-Rpass-analysis=kernel-resource-usage"]}
 # two waves per SIMD (a workgroup of 512 threads per compute unit) share its 512 registers

@@ -728,9 +728,12 @@ __global__ __launch_bounds__(64 * NW, 2) void paged_tile_kernel(PagedAttnArgs a)
   };
   // the row's reference, raised where a score of the tile is too far above
   auto refer = [&](const floatx16& s0, const floatx16& s1) __attribute__((always_inline)) {
-    float m = fmaxf(s0[0], s1[0]);
+    // (NaN is never the larger.  The start is hidden from the compiler, which otherwise takes the maximum of every tile, in front of
+    // the branch that few tiles take: a prompt of 8192 tokens, 32 heads, 624 us against 577.)
+    float m = -INFINITY;
+    asm volatile("" : "+v"(m));
 #pragma unroll
-    for (int i = 1; i < 16; ++i) m = fmaxf(m, fmaxf(s0[i], s1[i]));
+    for (int i = 0; i < 16; ++i) { m = s0[i] > m ? s0[i] : m; m = s1[i] > m ? s1[i] : m; }
     m *= a.scale_log2;
     m = fmaxf(m, __shfl_xor(m, 32));
     const float to = m > m_ref + Elem<T>::SLACK ? m - Elem<T>::SHIFT : m_ref;
