@@ -474,6 +474,8 @@ int32_t dsbd_paged_append(const dsbd_paged_kv* cache, int32_t n_rows, int32_t Hq
  * A row that sees nothing gets 0 and a lse of -Inf.  Slots behind a sequence's last token are never used, whatever they
  * hold, and neither is what a row does not see, NaN and Inf among it.  NaN in a row's query or in a key that it sees, and a
  * score of +Inf, make the row and its lse NaN; a score of -Inf has no weight.
+ * Scores, sums and outputs in fp32, numerators rounded to the type for the product with V (half a step of each).  They are
+ * up to 2^16 times as large as the final ones on the way: bf16 values up to 2^100 come out right, larger ones may overflow.
  * Sequences with lengths outside the bounds raise DSBD_FAULT_BOUNDS and get rows of 0 and -Inf; so do, for the tokens of
  * that page alone (they count as not there), page indices outside [0, n_pages).
  * Supported: D = 128 or 64, Hq % Hkv == 0.

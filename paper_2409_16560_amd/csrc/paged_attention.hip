@@ -33,14 +33,16 @@ typedef __attribute__((address_space(3))) v4i16 lds_v4i16;
 typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(1))) u32x4 gvec;
 
-// The two element types.  Softmax numerators are rounded to the type for the product with V; they are taken against a
-// reference exponent that trails the row's maximum: REF_SHIFT below it when it is set, raised when a score exceeds it by more than
-// SLACK.  bf16 has the exponent range for large slack (rare raises); f16 ends at 2^16, and starts to lose bits at 2^-14:
-// the shift keeps what is 2^-22 of the largest at full precision.
+// The two element types.  Softmax numerators are rounded to the type for the product with V (half a step of each term: what the
+// matrix units take); they are taken against a reference exponent that trails the row's maximum: SHIFT below it when it is set,
+// raised when a score exceeds it by more than SLACK.  bf16 has the exponent range for any slack; 2^16 is rarely passed and leaves the
+// sums of fp32, which end at 2^128, room for values of 2^100.  f16 ends at 2^16, and starts to lose bits at 2^-14: the shift keeps
+// what is 2^-22 of the largest at full precision.  MOST: a sum of 32 numerators that is within the slack (f16: that does not hold one
+// beyond the type's range).
 template <typename T> struct Elem;
 template <> struct Elem<__bf16> {
   typedef __bf16 x8 __attribute__((ext_vector_type(8)));
-  static constexpr float SLACK = 40.f, SHIFT = 0.f, MOST = 0x1p60f;
+  static constexpr float SLACK = 16.f, SHIFT = 0.f, MOST = 0x1p21f;
   static __device__ __forceinline__ floatx4 mfma(x8 a, x8 b, floatx4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
   static __device__ __forceinline__ floatx16 mfma(x8 a, x8 b, floatx16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
   static constexpr unsigned INF = 0x7f80u;

@@ -1,10 +1,12 @@
-"""Attention over pages with NaN and Inf in queries and keys that a row sees.  Outputs are checked as in
-test_gpu_paged_attention."""
+"""Attention over pages with values at the ends of their type: NaN and Inf in queries and keys that a row sees, values far above
+1 behind scores that climb.  Outputs are checked as in test_gpu_paged_attention."""
 import numpy as np
 import pytest
 import torch
 
 from oracle import paged as o_paged
+from test_gpu_paged_attention import check
+from test_gpu_paged_step import steep
 from test_gpu_qk_rows import BF16, F16, make_cache, np64, randn
 
 pytestmark = pytest.mark.gpu
@@ -67,3 +69,34 @@ def test_a_score_of_minus_infinity_counts_as_not_there(lens, Hq, dtype, D):
             w, wl, size = o_paged.attend(np64(q[r:r + 1]), k[:c + i + 1], v[:c + i + 1], there[:c + i + 1], c + i, D ** -0.5)
             tol = eps / 2 * (np.abs(w) + size) + 2e-4 * size + (c + n) * 2.0 ** -33 * size.max() + torch.finfo(dtype).smallest_normal
             assert (np.abs(np64(out[r]) - w[0]) <= tol[0])[1::2].all() and (np.abs(np64(lse[r]) - wl[0]) <= 2e-4)[1::2].all(), (s, i)
+
+
+def large_values(lens, Hq, Hk, far, rows):
+    """bf16 values about 2^100: the weighted sum stays in fp32's range, 2^128, while the reference trails the maximum.  Products and
+    sums of the scores are exact, as in test_gpu_paged_step."""
+    import paper_2409_16560_amd as dsbd
+    gen = torch.Generator().manual_seed(63)
+    cache, table, off, N = make_cache(gen, lens, 16, Hk, 128, BF16)
+    cache.k_pages.copy_(steep(gen, cache.k_pages.shape, BF16))
+    cache.v_pages.mul_(2.0 ** 100)
+    for s, (c, n) in enumerate(lens):
+        t = torch.arange(c + n)
+        up = ((t >= c - 9).float() if far else t.float() / (c + n)).mul(48).round().div(8).to(BF16).cuda()       # up to 6, times 4: 2^34.6
+        cache.k_pages[torch.from_numpy(table)[s, t // 16].long().cuda(), (t % 16).cuda(), :, 0] = up[:, None]
+    q = steep(gen, (N, Hq, 128), BF16).mul(1.0 / 64)
+    q[:, :, 0] = 4
+    out, lse, fault = dsbd.dsbd_paged_attention(cache, q, scale=1.0)
+    assert int(fault) == 0 and bool(out.isfinite().all())
+    check(cache, table, off, lens, q, out, lse, scale=1.0, rows=rows)
+
+
+@pytest.mark.parametrize("lens,Hq", SHAPES.values(), ids=SHAPES.keys())
+@pytest.mark.parametrize("far", [False, True], ids=["all along", "at the end"])
+def test_large_values_behind_climbing_scores(lens, Hq, far):
+    large_values(lens, Hq, 2, far, 10)
+
+
+@pytest.mark.parametrize("n", [1, 6])
+def test_large_values_where_a_wave_takes_step_after_step(n):
+    """Enough sequences to fill the device: none is split, and a wave sees the far ones in its third step."""
+    large_values([(380, n)] * 520, 8, 2, True, 2)
