@@ -495,10 +495,10 @@ typedef struct dsbd_logit_rules {
   const int32_t*  hist_off;      /* [n_trees+1] ascending: tokens in front of tree b's root (< 2^24 of them)  */
   const int32_t*  prompt_len;    /* [n_trees]; NULL: 0                                                        */
   /* [n_prompts] each */
-  const float*    repetition;    /* > 0 (a normal number): a token of the text: z > 0 ? z / r : z * r         */
+  const float*    repetition;    /* > 0: a token of the text: z > 0 ? z / r : z * r                           */
   const float*    frequency;     /* z -= frequency * (times the token was generated)                          */
   const float*    presence;      /* z -= presence, if it was generated                                        */
-  const float*    temperature;   /* > 0 (a normal number): z /= temperature, behind the biases                */
+  const float*    temperature;   /* > 0: z /= temperature, behind the biases                                  */
   /* biases: prompt p adds bias_value[i] to token bias_token[i], i in bias_off[p] .. bias_off[p+1]-1; of several entries
    * for one token the last counts */
   const int32_t*  bias_off;      /* [n_prompts+1] ascending, within [0, n_bias]                               */
