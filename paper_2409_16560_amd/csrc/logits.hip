@@ -108,6 +108,7 @@ __global__ __launch_bounds__(LG_BLOCK) void logits_kernel(LogitArgs a) {
   const int v0 = chunk * LG_CHUNK, nv = min(LG_CHUNK, a.V - v0);
   const bool counts = a.repetition || a.frequency || a.presence;
   int bad = 0;
+  bool known = true;               // the rows belong to nodes (one of row_node may belong to nothing: it is copied)
 
   // ---- rows on their way, one in front of the one in hand: the bits of a row's mask first, then the pieces that it does not
   // exclude as a whole
@@ -115,7 +116,7 @@ __global__ __launch_bounds__(LG_BLOCK) void logits_kernel(LogitArgs a) {
   Row now, next;
   auto load_bits = [&](int r, Row& to) {
     const uint32_t* mrow = nullptr;
-    if (a.mask) {
+    if (a.mask && known) {
       const int mi = a.mask_row ? a.mask_row[r] : r;
       if (mi >= a.n_masks) bad |= DSBD_FAULT_BOUNDS;
       else if (mi >= 0) mrow = a.mask + mi * a.mask_stride;
@@ -221,6 +222,8 @@ __global__ __launch_bounds__(LG_BLOCK) void logits_kernel(LogitArgs a) {
       return;
     }
   }
+  known = node0 >= base && node0 < base + n_b;
+  if (!known) bad |= DSBD_FAULT_TOPOLOGY;
   if (t >= 0 && (prompt < 0 || prompt >= a.n_prompts)) { prompt = -1; bad |= DSBD_FAULT_TOPOLOGY; }
   if (lo < 0 || hi < lo || hi > a.n_hist || hi - lo > (int)LG_TIMES) { lo = hi = 0; bad |= DSBD_FAULT_BOUNDS; }
   float rep = 1.f, freq = 0.f, pres = 0.f, temp = 1.f;
@@ -327,8 +330,7 @@ __global__ __launch_bounds__(LG_BLOCK) void logits_kernel(LogitArgs a) {
     if (q.x | q.y | q.z | q.w | b.x | b.y | b.z | b.w) rare |= 1u << k;
   }
   // ---- the rows
-  const bool known = node0 >= base && node0 < base + n_b;      // (a row of row_node may belong to nothing)
-  if (!known) { bad |= DSBD_FAULT_TOPOLOGY; rare = 0; }
+  if (!known) rare = 0;
   const Divisor by_temp(known ? temp : 1.f), by_rep(rep);
   for (int r = r0; r < r1; ++r) {
     if (r > r0 && r + 1 < r1) { load_bits(r + 1, next); load_row(r + 1, next); }
