@@ -305,12 +305,12 @@ PyObject* qk_norm_rope(PyObject*, PyObject* const* args, Py_ssize_t n) {
   void* const s = stream(args[8]);
   on_gpu(like);
   int32_t rc = DSBD_OK;
-  if (like.numel() > 0) {
+  const dsbd_rows *x[3], *y[3];      // (what has no heads is not there for the library)
+  for (int i = 0; i < 3; ++i) { x[i] = H[i] > 0 ? &from[i] : nullptr; y[i] = H[i] > 0 ? &to[i] : nullptr; }
+  if (N > 0 && D > 0 && (x[0] || x[1] || x[2])) {
     Py_BEGIN_ALLOW_THREADS
-    rc = dsbd_qk_norm_rope((int32_t)N, (int32_t)H[0], (int32_t)(in[1] ? H[1] : H[2]), (int32_t)D, element_type(like), in[0] ? &from[0] : nullptr,
-                           in[1] ? &from[1] : nullptr, in[2] ? &from[2] : nullptr, (const int32_t*)data(pos),
-                           args[4] != Py_None ? &prep : nullptr, in[0] ? &to[0] : nullptr, in[1] ? &to[1] : nullptr,
-                           in[2] ? &to[2] : nullptr, s);
+    rc = dsbd_qk_norm_rope((int32_t)N, (int32_t)H[0], (int32_t)(in[1] ? H[1] : H[2]), (int32_t)D, element_type(like), x[0], x[1], x[2],
+                           (const int32_t*)data(pos), args[4] != Py_None ? &prep : nullptr, y[0], y[1], y[2], s);
     Py_END_ALLOW_THREADS
   }
   if (rc != DSBD_OK) return PyLong_FromLong(rc);
@@ -354,7 +354,7 @@ PyObject* paged_append(PyObject*, PyObject* const* args, Py_ssize_t n) {
   void* const s = stream(args[8]);
   on_gpu(k);
   int32_t rc = DSBD_OK;
-  if (k.numel() > 0) {
+  if (N > 0) {
     Py_BEGIN_ALLOW_THREADS
     rc = dsbd_paged_append(&cache, (int32_t)N, (int32_t)Hq, (int32_t)Hkv, (int32_t)D, element_type(k), q ? &qr : nullptr, &kr, &vr,
                            (const int32_t*)data(pos), args[5] != Py_None ? &prep : nullptr, q ? &to : nullptr, fw, s);
