@@ -447,7 +447,7 @@ typedef struct dsbd_paged_kv {
   const int32_t* ctx_len;          /* [n_seqs] tokens in front of the new ones                               */
   const int32_t* q_off;            /* [n_seqs+1] ascending                                                   */
   int64_t        page_stride, token_stride, head_stride;   /* elements, multiples of 8                       */
-  int32_t        n_pages, page_size, table_stride, n_seqs;
+  int32_t        n_pages, page_size, table_stride, n_seqs;      /* page_size, n_seqs and max_len up to 2^30   */
   /* host-side bounds on the device data, checked on the device (DSBD_FAULT_BOUNDS): */
   int32_t        max_new;          /* >= new tokens of every sequence                                        */
   int32_t        max_len;          /* >= ctx_len + new tokens of every sequence                              */
@@ -508,7 +508,7 @@ typedef struct dsbd_logit_rules {
   const uint32_t* mask;          /* [n_masks,mask_stride], mask_stride >= (V+31)/32 words                     */
   const int32_t*  mask_row;      /* [n_rows] a row's mask, negative: none; NULL: row i has mask i             */
   int64_t         mask_stride;
-  int32_t         n_masks, n_hist, n_bias;
+  int32_t         n_masks, n_hist, n_bias;      /* n_hist and n_bias up to 2^30                              */
 } dsbd_logit_rules;
 
 /*

@@ -390,6 +390,8 @@ extern "C" int32_t dsbd_process_logits(const dsbd_forest* f, const int32_t* row_
   if (V < 1 || V > (1 << 30) || (dtype != DSBD_F32 && dtype != DSBD_BF16 && dtype != DSBD_F16)) return DSBD_ERR_UNSUPPORTED;
   if (f->n_prompts < 0 || f->n_trees < 0 || f->n_nodes < 0 || logits_stride < V || out_stride < V) return DSBD_ERR_INVALID;
   if (f->max_tree_nodes > DSBD_MAX_TREE_NODES) return DSBD_ERR_UNSUPPORTED;
+  // (the kernel's indices run past the ends by a few thousand before they are compared)
+  if (f->n_trees > (1 << 30) || rules->n_hist > (1 << 30) || rules->n_bias > (1 << 30)) return DSBD_ERR_UNSUPPORTED;
   if (!row_node && n_rows != f->n_nodes) return DSBD_ERR_INVALID;
   if (n_rows == 0) return DSBD_OK;
   if (!logits || !out || !f->tree_prompt || !f->tree_off || !f->parent || !f->token) return DSBD_ERR_INVALID;

@@ -32,7 +32,7 @@ static inline int32_t paged_check(const dsbd_paged_kv* c, int32_t n_rows, int32_
   if (c->n_seqs < 0 || c->n_pages < 0 || c->page_size < 1 || c->table_stride < 0 || c->max_new < 0 || c->max_len < 0 ||
       n_rows < 0 || Hkv < 1) return DSBD_ERR_INVALID;
   if (c->page_stride < 0 || c->token_stride < 0 || c->head_stride < 0) return DSBD_ERR_INVALID;
-  if (c->page_size > (1 << 30) || c->max_len > (1 << 30)) return DSBD_ERR_UNSUPPORTED;
+  if (c->page_size > (1 << 30) || c->max_len > (1 << 30) || c->n_seqs > (1 << 30)) return DSBD_ERR_UNSUPPORTED;
   if ((c->page_stride | c->token_stride | c->head_stride) & 7) return DSBD_ERR_UNSUPPORTED;
   if (n_rows == 0 || c->n_seqs == 0) return DSBD_OK;
   if (!c->ctx_len || !c->q_off) return DSBD_ERR_INVALID;
