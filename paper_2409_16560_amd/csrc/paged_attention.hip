@@ -99,8 +99,12 @@ struct Unit { int s, g, rb, part, nparts; };
 //   share is cut.
 //   (Three chunks of 600 to 2100 tokens behind up to 4100, 432 units for 256 workgroups: sequence by sequence, cut at the even share,
 //   228 us, longest first 211, cut a quarter later 195.)
-//   Fewer: even parts of at most `len` steps, where len is the shortest, to within a sixteenth, that makes no more parts than the
-//   device holds workgroups.
+//   (One sequence, whose blocks are in order as they are, or more than 64: one by one, cut at the even share.)
+//   Fewer: even parts of at most `len` tiles, where len is the shortest, to within a sixteenth, that makes no more parts than the
+//   device holds workgroups (or, of more than 64 sequences, one that certainly does); so units that are more than half of that many
+//   and alike are not cut.
+//   (Behind 8192 tokens, 32 heads on 8, cut at the even share, in two rounds, and as it is: 56 trees of 31 nodes 434 us, 384; a chunk
+//   of 1536 tokens 301, 256; three of 400 to 600 277, 234.)
 // False: nothing to do.
 __device__ __forceinline__ bool find_unit(const PagedAttnArgs& a, int slots, Unit& u, int& part_tiles) {
   const int lane = threadIdx.x & 63, rows = a.block_rows;
@@ -179,15 +183,23 @@ __device__ __forceinline__ bool find_unit(const PagedAttnArgs& a, int slots, Uni
   int len = 0x7fffffff;
   if (a.splits) {
     len = max((int)fmin(ceil(wave_sum(full) * a.Hkv / slots), 1e9), PA_MIN_STEPS);
-    if (2.0 * units <= slots) {
-      int hi = 2 * len;                        // enough: at most slots / 2 parts of that length, and one more for each unit
+    if (2.0 * units <= slots || (units <= slots && a.c.n_seqs <= 64)) {
+      auto fits = [&](int l) {
+        double n = 0.0;
+        for (int s0 = 0; s0 < a.c.n_seqs; s0 += 64) { measure(s0); n += (double)nrb * count(l); }
+        return wave_sum(n) * a.Hkv <= slots;
+      };
+      int hi = 2 * len;                        // enough for slots / 2 units: as many parts of that length, and one more for each
+      if (2.0 * units > slots) while (!fits(hi)) { len = hi; hi *= 2; }      // (ends where nothing is cut any more)
       while (hi - len > max(len / 16, 1)) {    // (at least 2 apart: mid lies between them)
         const int mid = (len + hi) / 2;
-        double n = 0.0;
-        for (int s0 = 0; s0 < a.c.n_seqs; s0 += 64) { measure(s0); n += (double)nrb * count(mid); }
-        if (wave_sum(n) * a.Hkv <= slots) hi = mid; else len = mid;
+        if (fits(mid)) hi = mid; else len = mid;
       }
       len = hi;
+    } else if (units <= slots) {
+      // (no search, which would look at all of them again and again: as many parts of that length as there is room for, and one more
+      // for each unit; 301 sequences, one of them long, 36 us, with a search 51)
+      len = max(len, (int)fmin(ceil(wave_sum(full) * a.Hkv / (slots - units)), 1e9));
     }
   }
   long long base = 0;
