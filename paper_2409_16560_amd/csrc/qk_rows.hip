@@ -131,7 +131,20 @@ __global__ __launch_bounds__(QR_BLOCK) void qk_rows_kernel(QkRowsArgs a) {
         if (!live) ss = 0.f;
 #pragma unroll
         for (int m = 1; m < LPR; m <<= 1) ss += __shfl_xor(ss, m);
-        const float inv = 1.0f / sqrtf(ss / (float)a.D + a.eps);
+        float inv = 1.0f / sqrtf(ss / (float)a.D + a.eps);
+        if constexpr (__is_same(T, __bf16)) {
+          // bf16 has fp32's exponents, its squares have not: such rows are brought near 1 (all lanes of the row agree)
+          if (!(ss <= 0x1p120f) || (ss < 0x1p-80f && a.eps < 0x1p-80f)) {
+            const float by = ss < 1.f ? 0x1p72f : 0x1p-72f;
+            ss = 0.f;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) { x[i] *= by; ss += x[i] * x[i]; }
+            if (!live) ss = 0.f;
+#pragma unroll
+            for (int m = 1; m < LPR; m <<= 1) ss += __shfl_xor(ss, m);
+            inv = 1.0f / sqrtf(ss / (float)a.D + a.eps * by * by);
+          }
+        }
         const char* const w = which == 0 ? a.q_weight : a.k_weight;
         float wt[16];
         if (w) {
