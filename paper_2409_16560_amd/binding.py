@@ -630,6 +630,7 @@ def rope_inv_freq(rot_dim, base=10000.0, scaling=None, factor=1.0, *, orig_len=0
             pair = lambda turns: rot_dim * math.log(orig_len / (2 * math.pi * turns)) / (2 * math.log(base))
             lo, hi = max(0, math.floor(pair(high))), min(rot_dim - 1, math.ceil(pair(low)))
             keep = 1.0 - ((i - lo) / max(hi - lo, 1e-3)).clamp(0.0, 1.0)
+            keep[orig_len * f <= 2 * math.pi * low] = 0.0      # (the first pair too, where no pair makes more)
             scale = 0.1 * math.log(factor) + 1.0 if factor > 1.0 else 1.0
         else:
             keep = ((orig_len * f / (2 * math.pi) - low) / (high - low)).clamp(0.0, 1.0)
