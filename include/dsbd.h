@@ -477,7 +477,8 @@ int32_t dsbd_paged_append(const dsbd_paged_kv* cache, int32_t n_rows, int32_t Hq
  * Scores, sums and outputs in fp32, numerators rounded to the type for the product with V (half a step of each).  They are
  * up to 2^16 times as large as the final ones on the way: bf16 values up to 2^100 come out right, larger ones may overflow.
  * Sequences with lengths outside the bounds raise DSBD_FAULT_BOUNDS and get rows of 0 and -Inf; so do, for the tokens of
- * that page alone (they count as not there), page indices outside [0, n_pages).
+ * that page alone (they count as not there), page indices outside [0, n_pages).  Offsets that do not ascend or leave the
+ * rows raise it too; what is written to the rows of such sequences, and to rows that two of them claim, is open.
  * Supported: D = 128 or 64, Hq % Hkv == 0.
  * Workspace: partial results of the sequences that are split, by the numbers in the arguments alone (not max_len).  Calls with
  * enough rows to fill the device split nothing and need the least, 256 bytes.
@@ -518,7 +519,7 @@ typedef struct dsbd_logit_rules {
  * is needed.  logits [n_rows,V] of type DSBD_F32, DSBD_BF16 or DSBD_F16, rows logits_stride elements apart; out [n_rows,V]
  * f32, rows out_stride apart, may be `logits` itself (f32, same stride).
  * Device-side problems: trees as in dsbd_forest_attention (the rows of a tree with unusable offsets, and of nodes behind a
- * tree's max_tree_nodes, are not written), a row_node outside the trees (DSBD_FAULT_TOPOLOGY: the row is copied), token ids outside
+ * tree's max_tree_nodes, are not written), a row_node outside the trees (DSBD_FAULT_TOPOLOGY: the row is copied, unmasked), token ids outside
  * [0, V) (DSBD_FAULT_TOKEN: ignored), offsets or a mask_row outside their arrays, a repetition or temperature that is not
  * above 0 (DSBD_FAULT_BOUNDS: that rule is left out).
  */

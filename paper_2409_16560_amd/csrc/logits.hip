@@ -8,7 +8,7 @@
 // the places of its 16 tokens that have a word or a bias as a bit per piece and streams row after row, without a barrier between rows of a tree, the
 // next row's loads on their way during a row's arithmetic.
 // Bound by HBM: logits are read once and written once, a piece that a mask excludes as a whole is not read at all: 191 rows of 128256
-// f32 with every rule 46.5 us, 198 MB at 4.3 TB/s (a large copy makes 5.2).  By latency where there are few rows: 7 us.
+// f32 with every rule 47.8 us, 198 MB at 4.1 TB/s (a large copy makes 5.2).  By latency where there are few rows: 7 us.
 #include "common.h"
 #include "paged.h"
 #include "topology_device.h"
@@ -70,7 +70,7 @@ template <> struct Piece<float> {
 // Quotients by one number: the product with its reciprocal, corrected by what it leaves of the dividend, which a fused multiply-add
 // knows exactly.  Off by half a step, or by 2^-130 where that is more (of numbers between 1 and 2, 5e9 quotients by 600 divisors are
 // the divided ones to the last bit); divisors far from 1, and dividends that the correction makes NaN (Inf), are divided.
-// (191 rows of 128256, f32, every rule: 48.6 us; everything divided 54.5.)
+// (191 rows of 128256, f32, every rule: 47.8 us; everything divided 54, products with a rounded reciprocal alone 46.5.)
 struct Divisor {
   float d, inv;
   bool near_1;
@@ -418,7 +418,7 @@ extern "C" int32_t dsbd_process_logits(const dsbd_forest* f, const int32_t* row_
           reinterpret_cast<uintptr_t>(out) % 16 == 0;
   a.n_chunks = (V + LG_CHUNK - 1) / LG_CHUNK;
   // A workgroup takes as many of a tree's nodes as leaves no more workgroups than the device holds at once: the text is scanned once
-  // for all of them (191 nodes of 8 trees behind texts of 8192 tokens, vocabulary 128256: 47 us; a node each 94, whole trees 111).  Rows of row_node may each have another tree: one row per workgroup.
+  // for all of them (191 nodes of 8 trees behind texts of 8192 tokens, vocabulary 128256: 47 us; a node each 94, whole trees 111, with quotients as products).  Rows of row_node may each have another tree: one row per workgroup.
   a.groups = n_rows;
   if (!row_node) {
     const long long fit = LG_SLOTS / a.n_chunks, most = (long long)f->n_trees * std::max(1, f->max_tree_nodes);

@@ -597,10 +597,10 @@ typedef __attribute__((address_space(3))) void lds_void;
 typedef const __attribute__((address_space(1))) void glb_cvoid;
 
 // NW: waves, 4 where 128 rows hold all of a sequence's (two workgroups per CU), 8 above (one, which fills a tile for twice the rows):
-// 8 trees of 31 nodes with 4 heads per KV head on 8192 tokens 71 us against 88; a prompt of 8192 tokens, 32 heads of 128, 638 us
-// against 582; three chunks of 600 to 2100 tokens 247 us against 234 (as they were ordered then).  RUNS: pages are whole multiples of
-// 8 tokens, so what a load instruction takes begins at one address and needs no place of its own in every lane (the prompt 616 us
-// against 655, in the form of 4 waves).
+// 8 trees of 31 nodes with 4 heads per KV head on 8192 tokens 78 us against 93; a prompt of 8192 tokens, 32 heads of 128, 599 us
+// against 556; three chunks of 600 to 2100 tokens, 4 heads per KV head, 199 us against 200.  RUNS: pages are whole multiples of 8
+// tokens, so what a load instruction takes begins at one address and needs no place of its own in every lane (the prompt 616 us
+// against 655, in an earlier form of 4 waves).
 template <typename T, int D, int NW, bool RUNS>
 __global__ __launch_bounds__(64 * NW, 2) void paged_tile_kernel(PagedAttnArgs a) {
   typedef typename Elem<T>::x8 x8;
@@ -989,7 +989,7 @@ Plan plan(const dsbd_paged_kv* c, int n_rows, int Hq, int Hkv, int D, PagedAttnA
   Plan p;
   const long long group = Hq / Hkv, most = (long long)std::min(c->max_new, n_rows) * group;     // rows of a sequence and KV head
   // (17 to 32 rows, in the wave-private kernel and in the tile kernel: 7 nodes for each of 32 sequences of 1024 to 8192 tokens, 4 heads per
-  // KV head, 141 us against 156; for each of 8 sequences of 8000 tokens 73 us against 66)
+  // KV head, 127 us against 142; for each of 8 sequences of 8000 tokens, where the rule takes the slower one, 71 us against 64)
   p.rows = most <= 16 ? 16 : most <= 32 ? 32 : most <= 128 ? 128 : 256;
   const bool wave = p.rows <= 32;
   const long long slots = wave ? PA_SLOTS : p.rows == 128 ? PA_TILE_SLOTS : PA_TILE_SLOTS / 2;

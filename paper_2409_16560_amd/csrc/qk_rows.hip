@@ -8,8 +8,8 @@
 // once, in 64 bits, and use them for all the heads they come by.
 // Bound by HBM where there are many rows: 8191 tokens, 32 + 32 heads of 128, f16, half of each head turned: 53.5 us, 268 MB at
 // 5.0 TB/s (a large copy makes 5.2); prompts of 300 to 2500 tokens, 40 + 40 + 40 heads, into pages: 77 us, 360 MB at 4.7.  By latency
-// where there are few: 248 nodes, 32 + 8 + 8 heads, 6 us.  The loads of the next head while one is worked on cost more (append 86 us)
-// than they hide, with 8 waves a SIMD; so do non-temporal stores (63 us instead of 53.5).
+// where there are few: q and k of 248 nodes, 32 + 8 heads, 6 us.  The loads of the next head while one is worked on cost more (append
+// 86 us) than they hide, with 4 waves a SIMD; so do non-temporal stores (63 us instead of 53.5).
 #include "common.h"
 #include "paged.h"
 #include <algorithm>
@@ -223,8 +223,8 @@ int32_t launch(QkRowsArgs& a, int32_t dtype, const dsbd_rows* q, const dsbd_rows
   if (a.n_rows == 0 || H == 0) return DSBD_OK;
   const int lpr = a.D <= 64 ? 4 : a.D <= 128 ? 8 : 16, rows = 64 / lpr, most = (H + rows - 1) / rows;
   // waves per token: all of its heads in one wave, so that the angles are worked out once, but for few tokens, which would
-  // leave the device empty (8 waves on each of 256 compute units): 248 nodes with 48 heads 7.8 us a call, 9.4 with one wave each;
-  // 64 tokens on their way into pages 9.0 and 10.4
+  // leave the device empty (8 waves on each of 256 compute units): 248 nodes with 40 heads 6.8 us a call, 9.7 with one wave each;
+  // 64 tokens with 48 heads on their way into pages 7.5 and 10.7
   a.parts = (int)std::max(1LL, std::min((long long)most, 2048LL / a.n_rows));
   const long long waves = (long long)a.n_rows * a.parts, wgs = (waves + QR_BLOCK / 64 - 1) / (QR_BLOCK / 64);
   if (wgs > 0x7fffffffLL) return DSBD_ERR_UNSUPPORTED;
