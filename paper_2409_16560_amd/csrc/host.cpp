@@ -174,8 +174,23 @@ struct Attr {
   ~Attr() { Py_DECREF(o); }
   Attr(const Attr&) = delete;
 };
-// A tensor attribute, or none.  (The handle keeps it alive for the call.)
-const at::Tensor* tensor_of(PyObject* o, const Name& n, bool optional = false) { return tensor(Attr(o, n).o, optional); }
+// The attributes that a call takes of its handles, until it returns: a handle may work one out on demand, or be given another by a
+// thread that runs meanwhile.
+struct Held {
+  PyObject* o[24];
+  int n = 0;
+  Held() = default;
+  Held(const Held&) = delete;
+  ~Held() { while (n) Py_DECREF(o[--n]); }
+};
+// A tensor attribute, or none.
+const at::Tensor* tensor_of(Held& held, PyObject* o, const Name& n, bool optional = false) {
+  EXPECT(held.n < (int)(sizeof(held.o) / sizeof(held.o[0])));
+  PyObject* const t = PyObject_GetAttr(o, n.s);
+  if (!t) throw python_error();
+  held.o[held.n++] = t;
+  return tensor(t, optional);
+}
 int64_t integer_of(PyObject* o, const Name& n) { return integer(Attr(o, n).o); }
 int32_t int32_of(PyObject* o, const Name& n) { return int32(Attr(o, n).o); }
 bool truth_of(PyObject* o, const Name& n) {
@@ -211,13 +226,13 @@ bool same_shape(const at::Tensor& a, int64_t n, int64_t H, int64_t D) {
   return a.dim() == 3 && a.size(0) == n && a.size(1) == H && a.size(2) == D;
 }
 
-dsbd_qk_prep prep_of(PyObject* o, const at::Tensor& like, int64_t Hq, int64_t Hk, int64_t D) {
+dsbd_qk_prep prep_of(Held& held, PyObject* o, const at::Tensor& like, int64_t Hq, int64_t Hk, int64_t D) {
   static const Name q_weight("q_weight"), k_weight("k_weight"), inv_freq("inv_freq"), eps("eps"), rot_scale("rot_scale"), norm("norm"),
       interleaved("interleaved");
   dsbd_qk_prep p;
-  const at::Tensor* const w[2] = {array(tensor_of(o, q_weight, true), like.scalar_type(), like),
-                                  array(tensor_of(o, k_weight, true), like.scalar_type(), like)};
-  const at::Tensor* const f = array(tensor_of(o, inv_freq, true), at::kDouble, like);
+  const at::Tensor* const w[2] = {array(tensor_of(held, o, q_weight, true), like.scalar_type(), like),
+                                  array(tensor_of(held, o, k_weight, true), like.scalar_type(), like)};
+  const at::Tensor* const f = array(tensor_of(held, o, inv_freq, true), at::kDouble, like);
   const int64_t heads[2] = {Hq, Hk};
   int64_t dims = 0;
   for (int i = 0; i < 2; ++i)
@@ -235,11 +250,11 @@ dsbd_qk_prep prep_of(PyObject* o, const at::Tensor& like, int64_t Hq, int64_t Hk
 }
 
 // The cache of a handle; `Hkv` and `D` as its pages have them.
-dsbd_paged_kv cache_of(PyObject* o, const at::Tensor& like, int64_t& Hkv, int64_t& D) {
+dsbd_paged_kv cache_of(Held& held, PyObject* o, const at::Tensor& like, int64_t& Hkv, int64_t& D) {
   static const Name k_pages("k_pages"), v_pages("v_pages"), page_table("page_table"), ctx_len("ctx_len"), q_off("q_off"),
       max_new("max_new"), max_len("max_len"), head_major("head_major");
-  const at::Tensor &k = *tensor_of(o, k_pages), &v = *tensor_of(o, v_pages), &table = *tensor_of(o, page_table);
-  const at::Tensor &ctx = *tensor_of(o, ctx_len), &off = *tensor_of(o, q_off);
+  const at::Tensor &k = *tensor_of(held, o, k_pages), &v = *tensor_of(held, o, v_pages), &table = *tensor_of(held, o, page_table);
+  const at::Tensor &ctx = *tensor_of(held, o, ctx_len), &off = *tensor_of(held, o, q_off);
   EXPECT(k.dim() == 4 && v.sizes() == k.sizes() && k.scalar_type() == like.scalar_type() && v.scalar_type() == like.scalar_type());
   EXPECT(k.numel() == 0 || (k.strides() == v.strides() && k.stride(3) == 1));
   EXPECT(table.dim() == 2 && off.numel() == ctx.numel() + 1 && table.size(0) == ctx.numel());
@@ -276,6 +291,7 @@ void on_gpu(const at::Tensor& t) { TORCH_CHECK_VALUE(t.is_cuda(), "the tensors m
 PyObject* qk_norm_rope(PyObject*, PyObject* const* args, Py_ssize_t n) {
   HANDLE_TH_ERRORS
   TORCH_CHECK_TYPE(n == 9, "qk_norm_rope takes 9 arguments");
+  Held held;
   const at::Tensor* const in[3] = {tensor(args[0], true), tensor(args[1], true), tensor(args[2], true)};
   const at::Tensor* const like_ = in[0] ? in[0] : in[1] ? in[1] : in[2];
   TORCH_CHECK_VALUE(like_ != nullptr, "no rows given");
@@ -301,7 +317,7 @@ PyObject* qk_norm_rope(PyObject*, PyObject* const* args, Py_ssize_t n) {
     to[i] = rows(made[i], like, true);
   }
   dsbd_qk_prep prep;
-  if (args[4] != Py_None) prep = prep_of(args[4], like, H[0], H[1], D);
+  if (args[4] != Py_None) prep = prep_of(held, args[4], like, H[0], H[1], D);
   void* const s = stream(args[8]);
   on_gpu(like);
   int32_t rc = DSBD_OK;
@@ -328,11 +344,12 @@ PyObject* qk_norm_rope(PyObject*, PyObject* const* args, Py_ssize_t n) {
 PyObject* paged_append(PyObject*, PyObject* const* args, Py_ssize_t n) {
   HANDLE_TH_ERRORS
   TORCH_CHECK_TYPE(n == 9, "paged_append takes 9 arguments");
+  Held held;
   const at::Tensor &k = *tensor(args[1]), &v = *tensor(args[2]);
   const at::Tensor *const q = tensor(args[3], true), *const given = tensor(args[6], true);
   TORCH_CHECK_VALUE(k.dim() == 3, "k is [n, heads, D]");
   int64_t Hkv, D;
-  const dsbd_paged_kv cache = cache_of(args[0], k, Hkv, D);
+  const dsbd_paged_kv cache = cache_of(held, args[0], k, Hkv, D);
   const int64_t N = k.size(0), Hq = q && q->dim() == 3 ? q->size(1) : 0;
   EXPECT(same_shape(k, N, Hkv, D) && same_shape(v, N, Hkv, D) && N <= INT32_MAX && Hkv <= INT32_MAX && D <= INT32_MAX);
   EXPECT(q == nullptr || (same_shape(*q, N, Hq, D) && Hq <= INT32_MAX));
@@ -349,7 +366,7 @@ PyObject* paged_append(PyObject*, PyObject* const* args, Py_ssize_t n) {
     to = rows(made, k, true);
   }
   dsbd_qk_prep prep;
-  if (args[5] != Py_None) prep = prep_of(args[5], k, Hq, Hkv, D);
+  if (args[5] != Py_None) prep = prep_of(held, args[5], k, Hq, Hkv, D);
   int32_t* const fw = fault_word(*tensor(args[7]), k);
   void* const s = stream(args[8]);
   on_gpu(k);
@@ -371,10 +388,11 @@ PyObject* paged_append(PyObject*, PyObject* const* args, Py_ssize_t n) {
 PyObject* paged_attention(PyObject*, PyObject* const* args, Py_ssize_t n) {
   HANDLE_TH_ERRORS
   TORCH_CHECK_TYPE(n == 10, "paged_attention takes 10 arguments");
+  Held held;
   const at::Tensor& q = *tensor(args[1]);
   TORCH_CHECK_VALUE(q.dim() == 3, "q is [n, heads, D]");
   int64_t Hkv, D;
-  const dsbd_paged_kv cache = cache_of(args[0], q, Hkv, D);
+  const dsbd_paged_kv cache = cache_of(held, args[0], q, Hkv, D);
   const int64_t N = q.size(0), Hq = q.size(1);
   EXPECT(q.size(2) == D && N <= INT32_MAX && Hq <= INT32_MAX && Hkv <= INT32_MAX && D <= INT32_MAX);
   const float scale = (float)number(args[2]);
@@ -425,9 +443,10 @@ PyObject* paged_attention(PyObject*, PyObject* const* args, Py_ssize_t n) {
 PyObject* paged_attention_workspace_bytes(PyObject*, PyObject* const* args, Py_ssize_t n) {
   HANDLE_TH_ERRORS
   TORCH_CHECK_TYPE(n == 3, "paged_attention_workspace_bytes takes 3 arguments");
+  Held held;
   static const Name k_pages("k_pages");
   int64_t Hkv, D;
-  const dsbd_paged_kv cache = cache_of(args[0], *tensor_of(args[0], k_pages), Hkv, D);
+  const dsbd_paged_kv cache = cache_of(held, args[0], *tensor_of(held, args[0], k_pages), Hkv, D);
   EXPECT(Hkv <= INT32_MAX && D <= INT32_MAX);
   return PyLong_FromSize_t(dsbd_paged_attention_workspace_bytes(&cache, int32(args[1]), int32(args[2]), (int32_t)Hkv, (int32_t)D));
   END_HANDLE_TH_ERRORS
@@ -437,6 +456,7 @@ PyObject* paged_attention_workspace_bytes(PyObject*, PyObject* const* args, Py_s
 PyObject* process_logits(PyObject*, PyObject* const* args, Py_ssize_t n) {
   HANDLE_TH_ERRORS
   TORCH_CHECK_TYPE(n == 7, "process_logits takes 7 arguments");
+  Held held;
   static const Name tree_prompt("tree_prompt"), tree_off("tree_off"), parent("parent"), token("token"), n_prompts("n_prompts"),
       n_trees("n_trees"), n_nodes("n_nodes"), max_tree_nodes("max_tree_nodes"), max_depth("max_depth"), max_prompt_trees("max_prompt_trees");
   static const Name hist("hist"), hist_off("hist_off"), prompt_len("prompt_len"), repetition("repetition"), frequency("frequency"),
@@ -448,8 +468,8 @@ PyObject* process_logits(PyObject*, PyObject* const* args, Py_ssize_t n) {
   const int64_t R = z.size(0), V = z.size(1);
   EXPECT(R <= INT32_MAX && V <= INT32_MAX && element_type(z) >= 0 && (V <= 1 || z.stride(1) == 1));
   dsbd_forest f;
-  const at::Tensor *const tp = array(tensor_of(fo, tree_prompt), at::kInt, z), *const to = array(tensor_of(fo, tree_off), at::kInt, z);
-  const at::Tensor *const pa = array(tensor_of(fo, parent), at::kInt, z), *const tk = array(tensor_of(fo, token, true), at::kInt, z);
+  const at::Tensor *const tp = array(tensor_of(held, fo, tree_prompt), at::kInt, z), *const to = array(tensor_of(held, fo, tree_off), at::kInt, z);
+  const at::Tensor *const pa = array(tensor_of(held, fo, parent), at::kInt, z), *const tk = array(tensor_of(held, fo, token, true), at::kInt, z);
   f.n_prompts = int32_of(fo, n_prompts); f.n_trees = int32_of(fo, n_trees); f.n_nodes = int32_of(fo, n_nodes);
   EXPECT(f.n_trees >= 0 && f.n_nodes >= 0 && f.n_prompts >= 0);
   EXPECT(tp->numel() == f.n_trees && to->numel() == (int64_t)f.n_trees + 1 && pa->numel() == f.n_nodes);
@@ -459,12 +479,12 @@ PyObject* process_logits(PyObject*, PyObject* const* args, Py_ssize_t n) {
   f.max_tree_nodes = int32_of(fo, max_tree_nodes); f.max_depth = int32_of(fo, max_depth); f.max_prompt_trees = int32_of(fo, max_prompt_trees);
   dsbd_logit_rules r;
   const auto ints = [&](const Name& name, int64_t count) {
-    const at::Tensor* const t = array(tensor_of(ro, name, true), at::kInt, z);
+    const at::Tensor* const t = array(tensor_of(held, ro, name, true), at::kInt, z);
     EXPECT(t == nullptr || count < 0 || t->numel() == count);
     return t;
   };
   const auto floats = [&](const Name& name, int64_t count) {
-    const at::Tensor* const t = array(tensor_of(ro, name, true), at::kFloat, z);
+    const at::Tensor* const t = array(tensor_of(held, ro, name, true), at::kFloat, z);
     EXPECT(t == nullptr || count < 0 || t->numel() == count);
     return t;
   };
